@@ -313,7 +313,7 @@ def _build(c, t):
         spans = [p.inp(t["spans"])] if "spans" in t else []
         blocks = [p.op(B.TN_OP_ATTN_BLOCK, [q, p.inp(t["k"][a:b]), p.inp(t["v"][a:b])] + slopes + spans, B.TN_F32, 1, d + 2 * heads, n_q_tiles=1,
                        n_kv_tiles=1, n_col_tiles=1, q_pos0=keys - 1, k_pos0=a, **rule) for a, b in _cut(keys, c["split"])]
-        outs = {"o": [p.op(B.TN_OP_ATTN_COMBINE, blocks, code, 1, d, head_dim=hd, hpg=heads, mode=1)]}
+        outs = {"o": [p.op(B.TN_OP_ATTN_COMBINE, blocks, code, 1, d, head_dim=hd, hpg=heads, finish=1)]}
         p.load()
         return p, outs
     rows = c["rows"]
@@ -321,14 +321,14 @@ def _build(c, t):
     spans = flat(p.grid(t["spans"], c["tile"], cols=False)) if "spans" in t else []
     par = dict(n_q_tiles=len(q), n_kv_tiles=len(k), n_col_tiles=len(q[0]), **rule)
     if c["op"] == "scores":
-        outs = {"o": [p.op(B.TN_OP_ATTN_BLOCK, flat(q) + flat(k) + flat(v) + slopes + spans, code, rows, d, mode=1, **par)]}
+        outs = {"o": [p.op(B.TN_OP_ATTN_BLOCK, flat(q) + flat(k) + flat(v) + slopes + spans, code, rows, d, finish=1, **par)]}
         p.load()
         return p, outs
     do = p.grid(t["do"], c["tile"])
     part = p.op(B.TN_OP_ATTN_BLOCK, flat(q) + flat(k) + flat(v) + slopes + spans, B.TN_F32, rows, d + 2 * heads, **par)
     r_, c_ = _cut(rows, c["tile"]), _cut(d, c["tile"])
-    o = [[p.op(B.TN_OP_ATTN_COMBINE, [part], code, r1 - r0, c1 - c0, row0=r0, col0=c0, head_dim=hd, hpg=heads, mode=1) for c0, c1 in c_] for r0, r1 in r_]
-    lse = [p.op(B.TN_OP_ATTN_COMBINE, [part], B.TN_F32, r1 - r0, heads, row0=r0, head_dim=hd, hpg=heads, mode=2) for r0, r1 in r_]
+    o = [[p.op(B.TN_OP_ATTN_COMBINE, [part], code, r1 - r0, c1 - c0, row0=r0, col0=c0, head_dim=hd, hpg=heads, finish=1) for c0, c1 in c_] for r0, r1 in r_]
+    lse = [p.op(B.TN_OP_ATTN_COMBINE, [part], B.TN_F32, r1 - r0, heads, row0=r0, head_dim=hd, hpg=heads, finish=2) for r0, r1 in r_]
     stats = [p.op(B.TN_OP_ATTN_BWD, o[i] + do[i] + [lse[i]], B.TN_F32, r1 - r0, 2 * heads, mode=4, n_q_tiles=1, n_col_tiles=len(c_), head_dim=hd)
              for i, (r0, r1) in enumerate(r_)]
     ins = flat(q) + flat(k) + flat(v) + flat(do) + stats + slopes + spans

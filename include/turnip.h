@@ -21,7 +21,7 @@
  *     matching *_destroy.  A memgraph owns a copy of everything it needs from the taskgraph, so
  *     the taskgraph may be destroyed after tn_compile.  A memgraph must outlive its executors.
  *   - All tensors are dense row-major 2-D tiles [rows, cols] of fp32 or bf16 elements, each
- *     stored contiguously (leading dimension = cols).
+ *     stored contiguously (leading dimension = cols).  Inputs that hold positions are 32-bit integers.
  */
 #ifndef TURNIP_H
 #define TURNIP_H
@@ -52,7 +52,7 @@ typedef struct tn_taskgraph tn_taskgraph;
 typedef struct tn_memgraph tn_memgraph;
 typedef struct tn_executor tn_executor;
 
-enum { TN_F32 = 0, TN_BF16 = 1 };    /* element type of a tensor */
+enum { TN_F32 = 0, TN_BF16 = 1, TN_I32 = 2 }; /* element type of a tensor; TN_I32: inputs that are positions or spans only */
 enum { TN_HOST = 0, TN_DEVICE = 1 }; /* where an input tensor lies when execution starts */
 
 /* Vertex kinds of a taskgraph.  Each is a pure function of its operands with a fixed summation
@@ -90,7 +90,12 @@ enum {
   TN_OP_SOFTMAX_STAT = 17,
   /* S, the SOFTMAX_STAT of its row block -> exp(scale * s - m) / l where visible, else 0;
    * k_pos0 is the position of this tile's first column. */
-  TN_OP_SOFTMAX_APPLY = 18
+  TN_OP_SOFTMAX_APPLY = 18,
+  /* Rotary embedding of whole heads in its other forms, and the norm of each head in the same pass (the
+   * choices of a decoder's queries and keys that TN_OP_ROPE leaves out); see HEAD_ROPE below. */
+  TN_OP_HEAD_ROPE = 19,     /* X[, gain [1, head_dim]][, positions TN_I32 [rows, 1]] -> of X's shape          */
+  TN_OP_HEAD_ROPE_BWD = 20, /* dY, X, gain[, positions] -> gradient of X (mode 0), sums of the gain's (mode 1) */
+  TN_OP_COL_SUM = 21        /* P_0..P_{n-1}, fp32 [r_i, cols] -> [1, cols]: the sum of all their rows          */
 };
 
 typedef struct {
@@ -149,7 +154,41 @@ typedef struct {
  *                                       follows, the transposes the matrix units want as row-major tiles:
  *                                       mode 1 -> K^T tiles, mode 2 -> Q^T tiles, mode 3 -> dO^T tiles, each
  *                                       [columns of the tile, rows of the tile], in the order of the grid
- *                                       they mirror. */
+ *                                       they mirror.
+ *   HEAD_ROPE    head_dim, pos0, rope_base, rotary_dim, rope_half, positions, norm, eps, rope_factor, rope_len0, rope_low,
+ *                rope_high, mode
+ *                                       X holds whole heads side by side (head_dim even, at most 1024).  norm != 0: every head x
+ *                                       of a row becomes x * rsqrt(sum x^2 / head_dim + eps) * gain first (the
+ *                                       gain operand is present then, of X's type).  Of its first rotary_dim (even; 0:
+ *                                       head_dim) elements the pairs i = 0 .. rotary_dim / 2 - 1 turn by position * f_i: elements
+ *                                       (2i, 2i + 1), or with rope_half != 0 (i, i + rotary_dim / 2); the others
+ *                                       stay.  Row r has position pos0 + r, or with positions != 0 pos0 +
+ *                                       positions[r].  f_i = rope_base^(-2i / rotary_dim); with rope_factor > 1
+ *                                       (0 or 1: none) f_i / rope_factor where rope_len0 is 0, else, t being the turns
+ *                                       rope_len0 * f_i / 2 pi, f_i where t >= rope_high, f_i / rope_factor where
+ *                                       t <= rope_low, and between them the two mixed linearly in t (rope_high > rope_low).
+ *                                       mode 1 (norm == 0): the inverse rotation, which is also the rotation's
+ *                                       gradient.  Sums, angles and sines are formed in 32 bits or more; one rounding.
+ *   HEAD_ROPE_BWD                       the same with norm != 0, X being the forward operand.  With u = the inverse rotation of
+ *                                       dY and n = x * rsqrt(..): mode 0 -> rsqrt(..) * (u * gain - n * mean(u * gain * n));
+ *                                       mode 1 -> fp32 [ceil(rows / 32), head_dim]: row i the sum of u * n over the
+ *                                       heads of rows 32 i .. 32 i + 31 (TN_OP_COL_SUM of them is the gain's gradient).
+ *   ATTN_BLOCK, ATTN_BWD: the score rule of the fields score_cap, slopes, spans.  Scores are
+ *                                       s = scale * q.k, then score_cap * tanh(s / score_cap) if score_cap > 0 (1e-6 .. 1e6), then
+ *                                       s - slope_h * |query position - key position| if slopes != 0.  A key is visible if causal allows
+ *                                       it and, with spans != 0, first <= key position < end for the row's span; a row
+ *                                       may see nothing.  Two more kinds of operands follow all others: with slopes != 0 one
+ *                                       fp32 [1, hpg], the slope of each head (constants: they have no gradient); with spans != 0 one
+ *                                       TN_I32 [rows, 2] per Q row tile, each row's first key position and the one behind
+ *                                       its last.  scale > 0, q_pos0 and k_pos0 in 0 .. 2^30.  Infinities and NaN in rows of K and V (Q, dO) a row does not see leave it alone.
+ *   ATTN_BLOCK   finish                 0: the partial described above; 1: the finished attention of the block, [rows, gw] in the
+ *                                       operands' type, zeros in a row that sees nothing
+ *   ATTN_COMBINE finish                 1: as 0, but a row that no partial has seen a key of gives zeros; 2 -> fp32 [rows, hpg]: the log-sum-exp
+ *                                       of the scores of rows [row0, row0 + rows), -inf for such a row (col0 == 0)
+ *   ATTN_BWD     mode 4                 n_q_tiles, n_col_tiles, head_dim; operands: the finished attention O (tiles like Q), the
+ *                                       dO tiles, one log-sum-exp (ATTN_COMBINE, finish 2) per Q row tile -> fp32 [q rows, 2*hpg]: what
+ *                                       mode 0 gives, with D = sum O dO, and without forming the scores again.  With a score rule
+ *                                       (trans_a == 0) modes 1 to 3 need no transposed grids.  The statistics of a rule come from mode 4. */
 typedef struct {
   int32_t nk;
   int32_t d;
@@ -172,6 +211,21 @@ typedef struct {
   int32_t v_trans;
   int32_t trans_a;
   int32_t mode;
+  /* HEAD_ROPE, HEAD_ROPE_BWD */
+  int32_t rotary_dim;
+  int32_t rope_half;
+  int32_t positions;
+  int32_t norm;
+  float rope_factor;
+  float rope_low;
+  float rope_high;
+  int32_t rope_len0;
+  /* ATTN_BLOCK, ATTN_BWD: the score rule */
+  float score_cap;
+  int32_t slopes;
+  int32_t spans;
+  /* ATTN_BLOCK, ATTN_COMBINE */
+  int32_t finish;
 } tn_op_params;
 
 /* ------------------------------------------------------------------------------------------ */
@@ -543,7 +597,8 @@ void tn_executor_destroy(tn_executor* ex);
 /* Copies every TN_DEVICE input from host_inputs[vid] (host memory, or GPU memory outside the
  * device buffer) to its compiled location and waits.  Must
  * precede each tn_execute of a graph that has such inputs (their locations are reused once they
- * are dead).  host_inputs has one entry per taskgraph vertex; entries of non-inputs are ignored. */
+ * are dead), unless the caller has seen to it that they lie there: written in place, or left from the run before by
+ * a memgraph that gives their ranges (tn_memgraph_vertex) to nothing else.  host_inputs has one entry per taskgraph vertex; entries of non-inputs are ignored. */
 tn_status tn_executor_place_inputs(tn_executor* ex, const void* const* host_inputs);
 
 /* Runs the memgraph to completion (Section 5; Appendix A).  host_inputs as above, read by load

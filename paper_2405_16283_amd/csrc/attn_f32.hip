@@ -15,8 +15,9 @@
 // fp32 reverse, 3 heads of 64, 160 positions, 2.8 ms -> 17 us (latency: a handful of workgroups); bf16, 32 heads
 // of 128, 347 queries against 1371 keys, 6.6 ms -> 0.10 ms.  (Reverse pass with the own rows by
 // way of LDS and all loads up to the first chunk issued before any is waited for: 18.1 -> 17.8 us, not kept.)
-#include "device.h"
-#include "kernels.h"
+#include "attn_rule.h"
+
+#include <climits>
 
 namespace tn {
 namespace {
@@ -151,7 +152,14 @@ __device__ __forceinline__ float row_sum(float v) {  // over the sixteen lanes o
   return v;
 }
 
-template <typename T, int HD>
+// A finished row of attention: sums over the sum of weights, zeros where nothing was seen.
+template <typename T>
+__device__ __forceinline__ void st4_finished(T* o, f32x4 v, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  st4(o, l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : v * inv);
+}
+
+template <typename T, int HD, bool RULE>
 __device__ __forceinline__ void attn_by_rows(DeviceTables t, const OpDesc& d) {
   const int* ax = t.aux + d.aux0;
   const int tq = ax[0], tk = ax[1], tc = ax[2], q_rows = ax[3], kv_rows = ax[4], nc = d.p.n_col_tiles, gw = nc * tc;
@@ -170,13 +178,23 @@ __device__ __forceinline__ void attn_by_rows(DeviceTables t, const OpDesc& d) {
       o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     float m = -INFINITY, l = 0.f;
-    const int seen = min(K.rows, d.p.q_pos0 + row - d.p.k_pos0 + 1);
+    int from = 0, seen = min(K.rows, d.p.q_pos0 + row - d.p.k_pos0 + 1);
+    float slope = 0.f;
+    if constexpr (RULE) {
+      const Rule rule(t, d);
+      rule.visible(row, from, seen);
+      slope = rule.slope(h);
+    }
 #pragma unroll 1
-    for (int k = 0; k < seen; ++k) {
+    for (int k = from; k < seen; ++k) {
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < C; ++i) s += dot4(q[i], K.at(k, c0 + 64 * i));
       s = row_sum(s);
+      if constexpr (RULE) {
+        float th;
+        s = Rule(t, d).score(s, slope, d.p.q_pos0 + row - d.p.k_pos0 - k, th);
+      }
       const float mn = fmaxf(m, s), ms = mn == -INFINITY ? 0.f : mn;
       const float alpha = __expf(m - ms), p = __expf(s - ms);
       m = mn;
@@ -184,6 +202,12 @@ __device__ __forceinline__ void attn_by_rows(DeviceTables t, const OpDesc& d) {
 #pragma unroll
       for (int i = 0; i < C; ++i) o[i] = o[i] * alpha + (d.p.v_trans ? V.at_t(k, c0 + 64 * i) : V.at(k, c0 + 64 * i)) * p;
     }
+    if constexpr (RULE)
+      if (ax[kRuleFinish]) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) st4_finished((T*)d.out + (size_t)row * gw + h * HD + c0 + 64 * i, o[i], l);
+        continue;
+      }
     float* out = (float*)d.out + (size_t)row * d.cols;
 #pragma unroll
     for (int i = 0; i < C; ++i)
@@ -196,8 +220,32 @@ __device__ __forceinline__ void attn_by_rows(DeviceTables t, const OpDesc& d) {
   }
 }
 
+// What the rows of a workgroup see together, of per-lane ranges (all lanes of the workgroup, lo == hi for nothing): keys before `begin` and from
+// `end` on nobody sees, those in [all_lo, all_hi) everybody does.  lds: 16 integers.
+struct Seen {
+  int begin, end, all_lo, all_hi;
+};
+__device__ __forceinline__ Seen seen_by_all(int lo, int hi, bool exists, int* lds) {
+  int v[4] = {exists && lo < hi ? lo : INT_MAX, exists ? -hi : 0, exists ? -lo : INT_MAX, exists ? hi : INT_MAX};  // minima all
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = min(v[k], __shfl_xor(v[k], off, 64));
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) lds[(threadIdx.x >> 6) * 4 + k] = v[k];
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = min(v[k], lds[w * 4 + k]);
+  __syncthreads();
+  return {v[0], -v[1], -v[2], v[3]};
+}
+
 // aux: [rows per Q tile, rows per K/V tile, columns per tile, q rows, kv rows]
-template <typename T, int HD>
+// RULE: scores go by a rule or rows are finished (attn_rule.h); the rest of aux is read.
+template <typename T, int HD, bool RULE>
 __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
@@ -229,18 +277,29 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   for (int j = 0; j < HD / 16; ++j) o[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  int end = kv_rows;  // keys above the diagonal of this workgroup's rows contribute nothing
+  int begin = 0, end = kv_rows;  // keys above the diagonal of this workgroup's rows contribute nothing
   if (causal) end = min(kv_rows, d.p.q_pos0 + qb * kRows + kRows - k_pos0);
+  int lo = 0, hi = 0;  // RULE: what this lane's query sees
+  Seen seen{};
+  float slope = 0.f;
+  if constexpr (RULE) {
+    const Rule rule(t, d);
+    if (row < q_rows) rule.visible(row, lo, hi);
+    seen = seen_by_all(lo, hi, row < q_rows, (int*)lds);
+    begin = seen.begin < seen.end ? seen.begin & ~(kRows - 1) : 0;
+    end = seen.end;
+    slope = rule.slope(h);
+  }
   // head size 64 has the registers to fetch the next chunk while one is multiplied; at 128 the second
   // workgroup of the compute unit covers the wait instead
   constexpr bool kAhead = HD == 64;
   constexpr int P = kAhead ? kPieces(HD) : kPieces(HD) / 2;
   f32x4 kn[P], vn[P];
-  if (kAhead && end > 0) {
-    load_chunk<T, HD, 0, P>(K, false, 0, kn);
-    load_chunk_vt<T, HD, 0, P>(V, v_trans, 0, vn);
+  if (kAhead && end > begin) {
+    load_chunk<T, HD, 0, P>(K, false, begin, kn);
+    load_chunk_vt<T, HD, 0, P>(V, v_trans, begin, vn);
   }
-  for (int kv0 = 0; kv0 < end; kv0 += kRows) {
+  for (int kv0 = begin; kv0 < end; kv0 += kRows) {
     __syncthreads();  // everybody is done with the chunk before
     if constexpr (!kAhead) {
       load_chunk<T, HD, 0, P>(K, false, kv0, kn);
@@ -259,7 +318,11 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
       load_chunk<T, HD, 0, P>(K, false, kv0 + kRows, kn);
       load_chunk_vt<T, HD, 0, P>(V, v_trans, kv0 + kRows, vn);
     }
-    if (causal && k_pos0 + kv0 + kRows - 1 > d.p.q_pos0 + qb * kRows && not_finite<HD, kRows>(vs)) odd = true;
+    if constexpr (RULE) {
+      if ((kv0 < seen.all_lo || min(kv0 + kRows, kv_rows) > seen.all_hi) && not_finite<HD, kRows>(vs)) odd = true;
+    } else {
+      if (causal && k_pos0 + kv0 + kRows - 1 > d.p.q_pos0 + qb * kRows && not_finite<HD, kRows>(vs)) odd = true;
+    }
     f32x4 s[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -282,7 +345,13 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int kv = kv0 + 16 * k + 4 * g + i;
-        if (mask && (kv >= kv_rows || (causal && k_pos0 + kv > qpos))) s[k][i] = -INFINITY;
+        if constexpr (RULE) {
+          float th;
+          s[k][i] = Rule(t, d).score(s[k][i], slope, qpos - k_pos0 - kv, th);
+          if (kv < lo || kv >= hi) s[k][i] = -INFINITY;
+        } else {
+          if (mask && (kv >= kv_rows || (causal && k_pos0 + kv > qpos))) s[k][i] = -INFINITY;
+        }
         mx = fmaxf(mx, s[k][i]);
       }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -314,10 +383,16 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
         if (j & 4) __builtin_amdgcn_sched_barrier(0);
       }
   }
-  if (causal && any_wave(odd, lds)) return attn_by_rows<T, HD>(t, d);
+  if ((causal || RULE) && any_wave(odd, lds)) return attn_by_rows<T, HD, RULE>(t, d);
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   if (row >= q_rows) return;
+  if constexpr (RULE)
+    if (ax[kRuleFinish]) {
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) st4_finished((T*)d.out + (size_t)row * gw + h * HD + 16 * j + 4 * g, o[j], l);
+      return;
+    }
   float* out = (float*)d.out + (size_t)row * d.cols;
 #pragma unroll
   for (int j = 0; j < HD / 16; ++j) {
@@ -335,8 +410,8 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   }
 }
 
-template <typename T, int HD, int MODE, typename Stat>
-__device__ __forceinline__ void attn_bwd_by_rows(const OpDesc& d, const Side<T, HD>& Q, const Side<T, HD>& K, const Side<T, HD>& V,
+template <typename T, int HD, int MODE, bool RULE, typename Stat>
+__device__ __forceinline__ void attn_bwd_by_rows(const DeviceTables& t, const OpDesc& d, const Side<T, HD>& Q, const Side<T, HD>& K, const Side<T, HD>& V,
                                                  const Side<T, HD>& D, int rb, int h, int gw, Stat stat) {
   constexpr int C = HD / 64;
   const Side<T, HD>&own = MODE == 1 ? Q : K, &other = MODE == 1 ? K : Q;
@@ -351,10 +426,22 @@ __device__ __forceinline__ void attn_bwd_by_rows(const OpDesc& d, const Side<T, 
       m2[i] = MODE == 1 ? D.at(row, c0 + 64 * i) : v_at(row, c0 + 64 * i);
       acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-    const int begin = MODE == 1 ? 0 : max(0, d.p.k_pos0 + row - d.p.q_pos0);
-    const int end = MODE == 1 ? min(K.rows, d.p.q_pos0 + row - d.p.k_pos0 + 1) : Q.rows;
+    int begin = MODE == 1 ? 0 : max(0, d.p.k_pos0 + row - d.p.q_pos0);
+    int end = MODE == 1 ? min(K.rows, d.p.q_pos0 + row - d.p.k_pos0 + 1) : Q.rows;
+    float slope = 0.f;
+    if constexpr (RULE) {
+      const Rule rule(t, d);
+      if (MODE == 1) rule.visible(row, begin, end);
+      else begin = 0;
+      slope = rule.slope(h);
+    }
 #pragma unroll 1
     for (int o = begin; o < end; ++o) {
+      if constexpr (RULE && MODE >= 2) {
+        int lo, hi;
+        Rule(t, d).visible(o, lo, hi);
+        if (row < lo || row >= hi) continue;
+      }
       float s = 0.f, dp = 0.f;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
@@ -362,8 +449,11 @@ __device__ __forceinline__ void attn_bwd_by_rows(const OpDesc& d, const Side<T, 
         if (MODE != 3) dp += dot4(m2[i], MODE == 1 ? v_at(o, c0 + 64 * i) : D.at(o, c0 + 64 * i));
       }
       const int q = MODE == 1 ? row : o;
-      float p = __expf(row_sum(s) * d.p.scale - stat(q, 0));
+      float z = row_sum(s) * d.p.scale, th = 0.f;
+      if constexpr (RULE) z = Rule(t, d).score(z, slope, d.p.q_pos0 + q - d.p.k_pos0 - (MODE == 1 ? o : row), th);
+      float p = __expf(z - stat(q, 0));
       if (MODE != 3) p *= (row_sum(dp) - stat(q, 1)) * d.p.scale;
+      if (RULE && MODE != 3) p *= 1.f - th * th;
 #pragma unroll
       for (int i = 0; i < C; ++i) acc[i] += (MODE == 3 ? D.at(o, c0 + 64 * i) : other.at(o, c0 + 64 * i)) * p;
     }
@@ -376,7 +466,7 @@ __device__ __forceinline__ void attn_bwd_by_rows(const OpDesc& d, const Side<T, 
 // Reverse pass.  Modes 0 (statistics) and 1 (dQ): the workgroup's own rows are queries, keys come in
 // chunks.  Modes 2 (dK) and 3 (dV): its own rows are keys, queries and their statistics come in chunks.
 // Scores are formed again from Q and K; p = exp(scale q.k - lse).
-template <typename T, int HD, int MODE>
+template <typename T, int HD, int MODE, bool RULE>
 __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const OpDesc& d, char* lds) {
   const int* ax = t.aux + d.aux0;
   const int tq = ax[0], tk = ax[1], tc = ax[2], q_rows = ax[3], kv_rows = ax[4];
@@ -402,6 +492,7 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
   float(*const x1)[HD + 4] = (float(*)[HD + 4])lds;                                             // K, or Q
   float(*const x2)[HD + 4] = (float(*)[HD + 4])(lds + sizeof(float) * kRows * (HD + 4));        // V, or dO
   float(*const xs)[2] = (float(*)[2])(lds + 2 * sizeof(float) * kRows * (HD + 4));              // statistics of the queries
+  int(*const sees)[2] = (int(*)[2])(xs + kRows);  // RULE, modes 2 and 3: what they see
   bool odd = false;  // a chunk on the diagonal that is not finite
 
   const int row = rb * kRows + w * 16 + n, rc = min(row, my_rows - 1);
@@ -419,8 +510,31 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
   int begin = 0, end = o_rows;
   if (causal && MODE <= 1) end = min(kv_rows, d.p.q_pos0 + rb * kRows + kRows - d.p.k_pos0);
   if (causal && MODE >= 2) begin = max(0, d.p.k_pos0 + rb * kRows - d.p.q_pos0);
+  int lo = 0, hi = 0;  // RULE, mode 1: what this lane's query sees
+  Seen seen{};
+  float slope = 0.f;
+  if constexpr (RULE) {
+    const Rule rule(t, d);
+    slope = rule.slope(h);
+    if (MODE == 1) {
+      if (row < my_rows) rule.visible(row, lo, hi);
+      seen = seen_by_all(lo, hi, row < my_rows, (int*)lds);
+      begin = seen.begin < seen.end ? seen.begin & ~(kRows - 1) : 0;
+      end = seen.end;
+    }
+  }
 
   for (int r0 = begin; r0 < end; r0 += kRows) {
+    bool all_see = true;  // RULE, modes 2 and 3: every query of the chunk sees every key of the workgroup
+    if constexpr (RULE && MODE >= 2) {
+      int ql = 0, qh = 0;  // lane by lane the chunk's queries; every wavefront finds the same
+      if (r0 + lane < q_rows) Rule(t, d).visible(r0 + lane, ql, qh);
+      const int k0 = rb * kRows, k1 = min(k0 + kRows, kv_rows);
+      if (!__any(max(ql, k0) < min(qh, k1))) continue;
+      all_see = __all(ql <= k0 && qh >= k1);
+      lo = ql;
+      hi = qh;
+    }
     f32x4 v1[kPieces(HD)], v2[kPieces(HD)];
     load_chunk<T, HD>(MODE <= 1 ? K : Q, false, r0, v1);
     load_chunk<T, HD>(MODE <= 1 ? V : D, MODE <= 1 && v_trans, r0, v2);
@@ -430,9 +544,15 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
     store_chunk<HD>(x1, v1);
     store_chunk<HD>(x2, v2);
     if (MODE >= 2 && threadIdx.x < 2 * kRows) xs[threadIdx.x / 2][threadIdx.x & 1] = sv;
+    if (RULE && MODE >= 2 && threadIdx.x < kRows) {
+      sees[threadIdx.x][0] = lo;
+      sees[threadIdx.x][1] = hi;
+    }
     __syncthreads();
     // some row of the workgroup and some row of the chunk do not see each other
-    if (MODE != 0 && causal && (MODE == 1 ? d.p.k_pos0 + r0 + kRows - 1 > d.p.q_pos0 + rb * kRows
+    if (RULE && (MODE == 1 ? r0 < seen.all_lo || min(r0 + kRows, kv_rows) > seen.all_hi : !all_see) && not_finite<kRows, HD>(MODE == 3 ? x2 : x1))
+      odd = true;
+    if (!RULE && MODE != 0 && causal && (MODE == 1 ? d.p.k_pos0 + r0 + kRows - 1 > d.p.q_pos0 + rb * kRows
                                           : d.p.k_pos0 + rb * kRows + kRows - 1 > d.p.q_pos0 + r0) &&
         not_finite<kRows, HD>(MODE == 3 ? x2 : x1))
       odd = true;
@@ -466,8 +586,13 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
         for (int i = 0; i < 4; ++i) {
           const int lr = 16 * (k + e) + 4 * g + i, o = r0 + lr;
           bool ok = o < o_rows;
-          if (causal) ok = ok && (MODE <= 1 ? d.p.k_pos0 + o <= pos : pos <= d.p.q_pos0 + o);
-          const float z = s[e][i] * scale;
+          float z = s[e][i] * scale, th = 0.f;
+          if constexpr (RULE) {
+            ok = MODE == 1 ? o >= lo && o < hi : row >= sees[lr][0] && row < sees[lr][1];
+            z = Rule(t, d).score(z, slope, MODE == 1 ? pos - d.p.k_pos0 - o : d.p.q_pos0 + o - pos, th);
+          } else {
+            if (causal) ok = ok && (MODE <= 1 ? d.p.k_pos0 + o <= pos : pos <= d.p.q_pos0 + o);
+          }
           if (MODE == 0) {
             s[e][i] = ok ? z : -INFINITY;
             if (!ok) dp[e][i] = 0.f;
@@ -476,6 +601,7 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
             float p = __expf(z - (MODE == 1 ? lse : xs[lr][0]));
             if (MODE == 1) p *= (dp[e][i] - Dr) * scale;
             if (MODE == 2) p *= (dp[e][i] - xs[lr][1]) * scale;
+            if (RULE && MODE != 3) p *= 1.f - th * th;
             wgt[i] = ok ? p : 0.f;
           }
         }
@@ -519,28 +645,31 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
     }
     return;
   }
-  if (causal && any_wave(odd, lds)) return attn_bwd_by_rows<T, HD, MODE>(d, Q, K, V, D, rb, h, gw, stat);
+  if ((causal || RULE) && any_wave(odd, lds)) return attn_bwd_by_rows<T, HD, MODE, RULE>(t, d, Q, K, V, D, rb, h, gw, stat);
   if (row >= my_rows) return;
   T* out = (T*)d.out + (size_t)row * gw + h * HD;
 #pragma unroll
   for (int j = 0; j < HD / 16; ++j) st4(out + 16 * j + 4 * g, acc[j]);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool RULE>
 __global__ void __launch_bounds__(256, 2) attn_bwd_f32_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   switch (d.p.mode) {
-    case 0: attn_bwd_f32_body<T, HD, 0>(t, d, lds); break;
-    case 1: attn_bwd_f32_body<T, HD, 1>(t, d, lds); break;
-    case 2: attn_bwd_f32_body<T, HD, 2>(t, d, lds); break;
-    default: attn_bwd_f32_body<T, HD, 3>(t, d, lds); break;
+    case 0:
+      if constexpr (!RULE) attn_bwd_f32_body<T, HD, 0, RULE>(t, d, lds);
+      break;
+    case 1: attn_bwd_f32_body<T, HD, 1, RULE>(t, d, lds); break;
+    case 2: attn_bwd_f32_body<T, HD, 2, RULE>(t, d, lds); break;
+    default: attn_bwd_f32_body<T, HD, 3, RULE>(t, d, lds); break;
   }
 }
 
 constexpr int fwd_lds(int hd) { return 4 * (kRows * (hd + 4) + hd * (kRows + 4)); }
 constexpr int bwd_lds(int hd) { return 4 * (2 * kRows * (hd + 4) + 2 * kRows); }
+constexpr int bwd_rule_lds(int hd) { return bwd_lds(hd) + 4 * 2 * kRows; }
 
 template <auto kernel>
 hipError_t launch(int lds, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
@@ -552,16 +681,17 @@ hipError_t launch(int lds, const DeviceTables& t, const Batch& b, int32_t max_bl
 
 }  // namespace
 
-hipError_t launch_attn_f32(bool reverse, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks,
+hipError_t launch_attn_f32(bool reverse, bool rule, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks,
                            hipStream_t s) {
   const bool bf = dtype == TN_BF16;
   if (head_dim != 64 && head_dim != 128) return hipErrorInvalidValue;
-#define TN_PICK(kernel, lds)                                                                                  \
-  (head_dim == 64 ? (bf ? launch<kernel<bf16_t, 64>>(lds(64), t, b, max_blocks, s)                            \
-                        : launch<kernel<float, 64>>(lds(64), t, b, max_blocks, s))                            \
-                  : (bf ? launch<kernel<bf16_t, 128>>(lds(128), t, b, max_blocks, s)                          \
-                        : launch<kernel<float, 128>>(lds(128), t, b, max_blocks, s)))
-  return reverse ? TN_PICK(attn_bwd_f32_kernel, bwd_lds) : TN_PICK(attn_f32_kernel, fwd_lds);
+#define TN_PICK(kernel, R, lds)                                                                                     \
+  (head_dim == 64 ? (bf ? launch<kernel<bf16_t, 64, R>>(lds(64), t, b, max_blocks, s)                               \
+                        : launch<kernel<float, 64, R>>(lds(64), t, b, max_blocks, s))                               \
+                  : (bf ? launch<kernel<bf16_t, 128, R>>(lds(128), t, b, max_blocks, s)                             \
+                        : launch<kernel<float, 128, R>>(lds(128), t, b, max_blocks, s)))
+  if (rule) return reverse ? TN_PICK(attn_bwd_f32_kernel, true, bwd_rule_lds) : TN_PICK(attn_f32_kernel, true, fwd_lds);
+  return reverse ? TN_PICK(attn_bwd_f32_kernel, false, bwd_lds) : TN_PICK(attn_f32_kernel, false, fwd_lds);
 #undef TN_PICK
 }
 

@@ -261,6 +261,7 @@ tn_status build_tables(tn_executor& ex) {
   std::vector<int32_t> aux;
   std::vector<double> theta;
   std::map<std::pair<int32_t, uint32_t>, int32_t> theta_at;
+  std::map<std::vector<uint32_t>, int32_t> turns_at;  // the same for the rotations of TN_OP_HEAD_ROPE
   std::map<std::vector<int64_t>, int32_t> row_keys;  // single-row products: B operands and mode -> key
   ex.info.assign(nv, VInfo{});
   auto addr = [&](int64_t m, uint64_t need, void** out) -> tn_status {
@@ -282,7 +283,7 @@ tn_status build_tables(tn_executor& ex) {
     d.rows = x.desc.rows;
     d.cols = x.desc.cols;
     d.n_in = (int32_t)x.operands.size();
-    d.p = x.p;
+    memcpy(&d.p, &x.p, sizeof d.p);
     d.trans_b = x.p.trans_b;
     d.dtype = x.operands.empty() ? x.desc.dtype : mg.v[x.operands[0]].desc.dtype;
     for (int64_t o : x.operands) {
@@ -294,6 +295,11 @@ tn_status build_tables(tn_executor& ex) {
     VInfo& vi = ex.info[m];
     vi.dtype = (int8_t)d.dtype;
     auto odesc = [&](int i) -> const tn_tensor_desc& { return mg.v[x.operands[i]].desc; };
+    auto add_rule = [&](const tn_op_params& p, int first) {  // operands of the rule begin at `first`
+      int32_t cap;
+      memcpy(&cap, &p.score_cap, 4);
+      aux.insert(aux.end(), {cap, p.slopes ? first : -1, p.spans ? first + (p.slopes ? 1 : 0) : -1, p.finish});
+    };
     switch (x.op_kind) {
       case TN_OP_GEMM: {
         if (x.p.trans_c) std::swap(d.rows, d.cols);  // the kernels work on the logical [rows, cols] product
@@ -365,6 +371,39 @@ tn_status build_tables(tn_executor& ex) {
         d.aux0 = (uint32_t)it->second;
         break;
       }
+      case TN_OP_HEAD_ROPE:
+      case TN_OP_HEAD_ROPE_BWD: {
+        const bool back = x.op_kind == TN_OP_HEAD_ROPE_BWD;
+        const tn_tensor_desc& xd = odesc(back ? 1 : 0);
+        vi.cls = !back ? LC_HEAD_ROPE : x.p.mode ? LC_HEAD_GAIN : LC_HEAD_ROPE_BWD;
+        vi.bytes = (back ? 2.0 : 1.0) * tensor_bytes(xd) + (double)x.bytes;
+        const int rd = x.p.rotary_dim ? x.p.rotary_dim : x.p.head_dim;
+        const float scaled[4] = {x.p.rope_factor, x.p.rope_low, x.p.rope_high, x.p.rope_base};
+        std::vector<uint32_t> key(6);
+        memcpy(key.data(), scaled, 16);
+        key[4] = (uint32_t)rd;
+        key[5] = (uint32_t)x.p.rope_len0;
+        auto it = turns_at.find(key);
+        if (it == turns_at.end()) {  // turns per position of every pair, in 64 bits: a position far out turns many times
+          it = turns_at.emplace(key, (int32_t)theta.size()).first;
+          for (int i = 0; i < rd / 2; ++i) {
+            const double f = std::pow((double)x.p.rope_base, -2.0 * i / rd) / 6.283185307179586476925;
+            double share = 1.0;  // of f as it is, the rest divided by the factor
+            if (x.p.rope_factor > 1.f)
+              share = x.p.rope_len0 == 0 ? 0.0 : std::min(1.0, std::max(0.0, (x.p.rope_len0 * f - x.p.rope_low) / ((double)x.p.rope_high - x.p.rope_low)));
+            theta.push_back(share == 1.0 ? f : f * share + f / (double)x.p.rope_factor * (1.0 - share));
+          }
+        }
+        aux.insert(aux.end(), {it->second, rd, x.p.rope_half != 0, x.p.norm != 0, x.p.positions != 0, xd.rows, xd.cols});
+        break;
+      }
+      case TN_OP_COL_SUM:
+        vi.cls = LC_COL_SUM;
+        for (int i = 0; i < d.n_in; ++i) {
+          aux.push_back(odesc(i).rows);
+          vi.bytes += (double)tensor_bytes(odesc(i));
+        }
+        break;
       case TN_OP_ATTN_BLOCK: {
         const int nq = x.p.n_q_tiles, nkv = x.p.n_kv_tiles, nc = x.p.n_col_tiles, hd = x.p.head_dim;
         const int tq = odesc(0).rows, tk = odesc(nq * nc).rows, tc = odesc(0).cols;
@@ -384,6 +423,14 @@ tn_status build_tables(tn_executor& ex) {
           if (odesc(c).cols != tc) return fail(TN_ERR_SHAPE, "attn_block %lld: column tiles are not uniform", (long long)m);
         if (hd != 64 && hd != 128) return fail(TN_ERR_SHAPE, "attn_block %lld: head_dim must be 64 or 128", (long long)m);
         aux.insert(aux.end(), {tq, tk, tc, q_rows, kv_rows});
+        if (has_rule(x.p) || x.p.finish) {
+          add_rule(x.p, (nq + 2 * nkv) * nc);
+          vi.cls = LC_ATTN_RULE_F32;
+          vi.head_dim = (int16_t)hd;
+          vi.flops = 4.0 * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
+          vi.bytes = (q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
+          break;
+        }
         // the MFMA kernel wants V^T tiles, whole heads inside one column tile, 64-key chunks inside
         // one row tile, 16-byte chunks that do not straddle anything, and a positive scale (it takes
         // the row maximum before scaling)
@@ -395,7 +442,7 @@ tn_status build_tables(tn_executor& ex) {
         break;
       }
       case TN_OP_ATTN_COMBINE:
-        vi.cls = LC_ATTN_COMBINE;
+        vi.cls = x.p.finish == 2 ? LC_ATTN_LSE : x.p.finish ? LC_ATTN_JOIN : LC_ATTN_COMBINE;
         d.dtype = x.desc.dtype;
         vi.dtype = (int8_t)d.dtype;
         vi.bytes = x.bytes + d.n_in * ((double)d.rows * d.cols * 4.0);
@@ -446,6 +493,17 @@ tn_status build_tables(tn_executor& ex) {
         break;
       case TN_OP_ATTN_BWD: {
         const int nq = x.p.n_q_tiles, nkv = x.p.n_kv_tiles, nc = x.p.n_col_tiles, hd = x.p.head_dim;
+        if (x.p.mode == 4) {
+          for (int c = 0; c < nc; ++c)
+            if (odesc(c).cols != odesc(0).cols) return fail(TN_ERR_SHAPE, "attn_bwd %lld: column tiles are not uniform", (long long)m);
+          for (int r = 0; r + 1 < nq; ++r)
+            if (odesc(r * nc).rows != odesc(0).rows || odesc((r + 1) * nc).rows > odesc(0).rows)
+              return fail(TN_ERR_SHAPE, "attn_bwd %lld: Q row tiles are not uniform", (long long)m);
+          aux.insert(aux.end(), {odesc(0).rows, 0, odesc(0).cols, d.rows, 0});
+          vi.cls = LC_ATTN_STATS;
+          vi.bytes = 2.0 * d.rows * nc * odesc(0).cols * elem_bytes(d.dtype);
+          break;
+        }
         const int tq = odesc(0).rows, tk = odesc(nq * nc).rows, tc = odesc(0).cols;
         int q_rows = 0, kv_rows = 0;
         for (int r = 0; r < nq; ++r) {
@@ -462,6 +520,14 @@ tn_status build_tables(tn_executor& ex) {
           if (odesc(c).cols != tc) return fail(TN_ERR_SHAPE, "attn_bwd %lld: column tiles are not uniform", (long long)m);
         if (hd != 64 && hd != 128) return fail(TN_ERR_SHAPE, "attn_bwd %lld: head_dim must be 64 or 128", (long long)m);
         aux.insert(aux.end(), {tq, tk, tc, q_rows, kv_rows});
+        if (has_rule(x.p)) {
+          add_rule(x.p, 2 * (nq + nkv) * nc + nq);
+          vi.cls = LC_ATTN_BWD_RULE;
+          vi.head_dim = (int16_t)hd;
+          vi.flops = (x.p.mode == 3 ? 4.0 : 6.0) * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
+          vi.bytes = (2.0 * q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
+          break;
+        }
         // the MFMA kernel wants plain V tiles, the transposed grid (except for the statistics), whole
         // heads inside one column tile, 64-row chunks inside one row tile, 8-row groups that
         // straddle nothing, and a positive scale (the row maximum is taken before scaling)
@@ -623,7 +689,9 @@ int family_of(int cls) {
     case LC_ATTN_BWD_BF16:
     case LC_ATTN_BWD_BF16_DQ:
     case LC_ATTN_BWD_BF16_DK:
-    case LC_ATTN_BWD_BF16_DV: return 1;
+    case LC_ATTN_BWD_BF16_DV:
+    case LC_ATTN_RULE_F32:
+    case LC_ATTN_BWD_RULE: return 1;
     default: return 2;
   }
 }

@@ -16,7 +16,7 @@ namespace tn {
 void set_error(const char* fmt, ...);
 tn_status fail(tn_status code, const char* fmt, ...);
 
-inline uint64_t elem_bytes(int32_t dtype) { return dtype == TN_F32 ? 4u : 2u; }
+inline uint64_t elem_bytes(int32_t dtype) { return dtype == TN_BF16 ? 2u : 4u; }
 inline uint64_t tensor_bytes(const tn_tensor_desc& d) {
   return (uint64_t)d.rows * (uint64_t)d.cols * elem_bytes(d.dtype);
 }
@@ -58,6 +58,9 @@ struct MemGraph {
   std::vector<int64_t> order;
   tn_mg_stats stats{};
 };
+
+// Whether attention goes by a score rule or leaves finished rows, which the plain kernels do not do.
+inline bool has_rule(const tn_op_params& p) { return p.score_cap > 0.f || p.slopes || p.spans; }
 
 // Shape/type rules of the vertex kinds; returns TN_OK or sets the error text.
 tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, const tn_vid* in,

@@ -9,11 +9,25 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <cstddef>
 #include <cstdint>
 
 #include "turnip.h"
 
 namespace tn {
+
+// What descriptors hold of a vertex's parameters: the fields up to `mode`.  Those behind it belong to a few kinds, which get them
+// by way of the auxiliary integers: descriptors stay as small as they were, and a static table holds as many of them.
+struct KernelParams {
+  int32_t nk, d;
+  float eps;
+  int32_t pos0, col0, head_dim;
+  float rope_base;
+  int32_t n_q_tiles, n_kv_tiles, n_col_tiles, q_pos0, k_pos0, causal;
+  float scale;
+  int32_t row0, hpg, trans_b, trans_c, v_trans, trans_a, mode;
+};
+static_assert(sizeof(KernelParams) == offsetof(tn_op_params, rotary_dim) && offsetof(KernelParams, mode) == offsetof(tn_op_params, mode), "the same fields");
 
 // One kernel-call vertex, as the kernels see it.
 struct OpDesc {
@@ -25,7 +39,7 @@ struct OpDesc {
   int32_t nblocks;  // workgroups this vertex needs in its launch class
   int32_t dtype;    // storage type of its non-statistics operands (TN_F32 / TN_BF16)
   int32_t trans_b;  // gemm: B tiles are stored [cols, K]
-  tn_op_params p;
+  KernelParams p;
 };
 
 // Lets `kernel` be launched with `bytes` of dynamic LDS on the current GPU, where that is more than 64 KiB: a GPU is told of it
@@ -67,6 +81,15 @@ enum LaunchClass {
   LC_ZERO,           // clears a tensor: the start of a sum's output
   LC_SOFTMAX_STAT,   // row maximum and sum of exponentials over the score tiles of a row block
   LC_SOFTMAX_APPLY,  // probabilities of one score tile
+  LC_HEAD_ROPE,      // norm and rotation of heads, any size
+  LC_HEAD_ROPE_BWD,  // gradient of their input
+  LC_HEAD_GAIN,      // sums of their gain's gradient
+  LC_COL_SUM,
+  LC_ATTN_RULE_F32,  // attention with a score rule or finished rows, fp32 products
+  LC_ATTN_BWD_RULE,  // its gradients, fp32 products
+  LC_ATTN_STATS,     // their statistics from O, dO and the log-sum-exp
+  LC_ATTN_JOIN,      // combine with finish 1
+  LC_ATTN_LSE,       // combine with finish 2
   LC_COUNT,
   // Not a class of its own for grouping: 128x128 tiles with two workgroups per CU, a form for launches of either of the two above.
   LC_GEMM_BF16_PAIRED
@@ -175,8 +198,18 @@ struct RowVertex {
 hipError_t launch_gemm_rows(int dtype, const DeviceTables& t, uint32_t base, const RowVertex* rows, int n, int32_t max_blocks,
                             hipStream_t stream);
 
-// LC_ATTN_F32 (reverse == false) and LC_ATTN_BWD: attn_f32.hip.
-hipError_t launch_attn_f32(bool reverse, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks,
+// Auxiliary integers of attention vertices: rows per Q tile, rows per K/V tile, columns per tile, q rows, kv rows; those with a score
+// rule or finished rows have these behind them.
+enum { kRuleCap = 5, kRuleSlopes, kRuleSpans, kRuleFinish, kRuleAux };  // bits of score_cap; operand of the slopes and of the first spans, or -1
+
+// LC_HEAD_ROPE to LC_COL_SUM: heads.hip.  Auxiliary integers of the first three (of LC_COL_SUM: rows per operand):
+enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadAux };
+constexpr int kGainRows = 32;  // rows to a sum of the gain's gradient
+int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux);
+hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
+
+// LC_ATTN_F32 and LC_ATTN_RULE_F32 (reverse == false), LC_ATTN_BWD and LC_ATTN_BWD_RULE: attn_f32.hip.
+hipError_t launch_attn_f32(bool reverse, bool rule, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks,
                            hipStream_t stream);
 
 }  // namespace tn

@@ -368,7 +368,8 @@ __global__ void __launch_bounds__(256) rope_kernel(DeviceTables t, Batch b) {
 __host__ __device__ __forceinline__ bool combine_by_four(const OpDesc& d) {
   return d.cols % 4 == 0 && d.p.col0 % 4 == 0 && d.p.head_dim % 4 == 0;
 }
-template <typename T>
+// JOIN: a row of which no partial has seen a key gives zeros.
+template <typename T, bool JOIN>
 __global__ void __launch_bounds__(256) attn_combine_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
@@ -383,6 +384,7 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(DeviceTables t, Batch
     const bool wide = (ldp & 3) == 0;  // rows of a partial are 16-byte aligned
     float mstar = -INFINITY;
     for (int j = 0; j < d.n_in; ++j) mstar = fmaxf(mstar, ((const float*)t.ptrs[d.ptr0 + j])[r + gw + h]);
+    if (JOIN && mstar == -INFINITY) mstar = 0.f;
     float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
 #pragma unroll 4
     for (int j = 0; j < d.n_in; ++j) {
@@ -400,6 +402,7 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(DeviceTables t, Batch
       for (int k = 0; k < 4; ++k) num[k] += v[k] * w;
       den += p[r + gw + hpg + h] * w;
     }
+    if (JOIN && den == 0.f) den = 1.f;
     T* out = (T*)d.out + (size_t)row * d.cols + c;
     if constexpr (sizeof(T) == 2) {
       uint2 u;
@@ -417,6 +420,7 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(DeviceTables t, Batch
   const size_t r = (size_t)(d.p.row0 + row) * ldp;
   float mstar = -INFINITY;
   for (int j = 0; j < d.n_in; ++j) mstar = fmaxf(mstar, ((const float*)t.ptrs[d.ptr0 + j])[r + gw + h]);
+  if (JOIN && mstar == -INFINITY) mstar = 0.f;
   float num = 0.f, den = 0.f;
   for (int j = 0; j < d.n_in; ++j) {
     const float* p = (const float*)t.ptrs[d.ptr0 + j];
@@ -424,7 +428,59 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(DeviceTables t, Batch
     num += p[r + col] * w;
     den += p[r + gw + hpg + h] * w;
   }
+  if (JOIN && den == 0.f) den = 1.f;
   st((T*)d.out + (size_t)row * d.cols + c, num / den);
+}
+
+// The log-sum-exp of a row and head over the partials of its block, -inf where none has seen a key.
+__global__ void __launch_bounds__(256) attn_lse_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (int64_t)d.rows * d.cols) return;
+  const int row = (int)(id / d.cols), h = (int)(id % d.cols), hpg = d.p.hpg, gw = d.p.head_dim * hpg;
+  const size_t at = (size_t)(d.p.row0 + row) * (gw + 2 * hpg) + gw + h;
+  float m = -INFINITY;
+  for (int j = 0; j < d.n_in; ++j) m = fmaxf(m, ((const float*)t.ptrs[d.ptr0 + j])[at]);
+  const float ms = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  for (int j = 0; j < d.n_in; ++j) {
+    const float* p = (const float*)t.ptrs[d.ptr0 + j] + at;
+    l += p[hpg] * __expf(p[0] - ms);
+  }
+  ((float*)d.out)[id] = ms + logf(l);
+}
+
+// Statistics of the reverse pass from what the forward pass left: per row and head the log-sum-exp as it is, and
+// D = sum_k p dp = sum_k p (dO . v_k) = dO . O.  Sixteen lanes to a row and head.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_stats_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  const int* ax = t.aux + d.aux0;
+  const int tq = ax[0], tc = ax[2], nc = d.p.n_col_tiles, hd = d.p.head_dim, hpg = nc * tc / hd;
+  const int64_t id = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (id >= (int64_t)d.rows * hpg) return;
+  const int row = (int)(id / hpg), h = (int)(id % hpg), lane = threadIdx.x & 15;
+  void* const* O = t.ptrs + d.ptr0;
+  void* const* dO = O + d.p.n_q_tiles * nc;
+  float sum = 0.f;
+  if (tc % 4 == 0 && hd % 4 == 0) {
+    for (int c = lane * 4; c < hd; c += 64) {
+      const f32x4 x = ld4(tile_elem<T>(O, nc, tq, tc, row, h * hd + c)), y = ld4(tile_elem<T>(dO, nc, tq, tc, row, h * hd + c));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum = fmaf(x[k], y[k], sum);
+    }
+  } else {
+    for (int c = lane; c < hd; c += 16) sum = fmaf(ld(tile_elem<T>(O, nc, tq, tc, row, h * hd + c)), ld(tile_elem<T>(dO, nc, tq, tc, row, h * hd + c)), sum);
+  }
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) sum += __shfl_xor(sum, off, 64);
+  if (lane) return;
+  const int rt = row / tq;
+  float* out = (float*)d.out + (size_t)row * (2 * hpg);
+  out[h] = ((const float*)dO[d.p.n_q_tiles * nc + rt])[(size_t)(row - rt * tq) * hpg + h];
+  out[hpg + h] = sum;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1261,6 +1317,13 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
     case LC_RMS_APPLY: return cdiv((int64_t)d.rows * cdiv(d.cols, 8), 256);
     case LC_ROPE:
       return rope_whole_heads(d) ? cdiv((int64_t)d.rows * (d.p.head_dim / 8), 256) : cdiv((int64_t)d.rows * (d.cols / 2), 256);
+    case LC_HEAD_ROPE:
+    case LC_HEAD_ROPE_BWD:
+    case LC_HEAD_GAIN:
+    case LC_COL_SUM: return head_blocks(cls, d, aux);
+    case LC_ATTN_STATS: return cdiv((int64_t)d.rows * (d.p.n_col_tiles * aux[d.aux0 + 2] / d.p.head_dim), 16);
+    case LC_ATTN_LSE: return cdiv((int64_t)d.rows * d.cols, 256);
+    case LC_ATTN_RULE_F32:
     case LC_ATTN_F32: {
       const int gw = d.p.n_col_tiles * aux[d.aux0 + 2];
       return (gw / d.p.head_dim) * cdiv(aux[d.aux0 + 3], 64);
@@ -1269,6 +1332,7 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
       const int gw = d.p.n_col_tiles * aux[d.aux0 + 2];
       return (gw / d.p.head_dim) * cdiv(aux[d.aux0 + 3], 128);
     }
+    case LC_ATTN_JOIN:
     case LC_ATTN_COMBINE: return cdiv((int64_t)d.rows * d.cols / (combine_by_four(d) ? 4 : 1), 256);
     case LC_SILU_MUL:
     case LC_ADD:
@@ -1279,6 +1343,7 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
     case LC_SOFTMAX_APPLY: return cdiv((int64_t)d.rows * cdiv(d.cols, 8), 256);
     case LC_RMS_BWD_STAT: return cdiv(d.rows, 4);
     case LC_RMS_BWD_APPLY: return cdiv((int64_t)d.rows * cdiv(d.cols, 8), 256);
+    case LC_ATTN_BWD_RULE:
     case LC_ATTN_BWD: {
       const int gw = d.p.n_col_tiles * aux[d.aux0 + 2];
       return (gw / d.p.head_dim) * cdiv(aux[d.aux0 + (d.p.mode <= 1 ? 3 : 4)], 64);
@@ -1353,7 +1418,16 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
     case LC_RMS_STAT: TN_LAUNCH_T(rms_stat_kernel); break;
     case LC_RMS_APPLY: TN_LAUNCH_T(rms_apply_kernel); break;
     case LC_ROPE: TN_LAUNCH_T(rope_kernel); break;
-    case LC_ATTN_COMBINE: TN_LAUNCH_T(attn_combine_kernel); break;
+    case LC_ATTN_COMBINE:
+      if (bf) hipLaunchKernelGGL((attn_combine_kernel<bf16_t, false>), grid, wg, 0, s, t, b);
+      else hipLaunchKernelGGL((attn_combine_kernel<float, false>), grid, wg, 0, s, t, b);
+      break;
+    case LC_ATTN_JOIN:
+      if (bf) hipLaunchKernelGGL((attn_combine_kernel<bf16_t, true>), grid, wg, 0, s, t, b);
+      else hipLaunchKernelGGL((attn_combine_kernel<float, true>), grid, wg, 0, s, t, b);
+      break;
+    case LC_ATTN_LSE: hipLaunchKernelGGL(attn_lse_kernel, grid, wg, 0, s, t, b); break;
+    case LC_ATTN_STATS: TN_LAUNCH_T(attn_stats_kernel); break;
     case LC_SILU_MUL:
       if (bf) hipLaunchKernelGGL((ewise2_kernel<bf16_t, true>), grid, wg, 0, s, t, b);
       else hipLaunchKernelGGL((ewise2_kernel<float, true>), grid, wg, 0, s, t, b);
@@ -1386,8 +1460,14 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
     case LC_ATTN_BWD_BF16_DK: TN_LAUNCH_ATTN_BWD(2); break;
     case LC_ATTN_BWD_BF16_DV: TN_LAUNCH_ATTN_BWD(3); break;
 #undef TN_LAUNCH_ATTN_BWD
-    case LC_ATTN_BWD: return launch_attn_f32(true, dtype, head_dim, t, b, max_blocks, s);
-    case LC_ATTN_F32: return launch_attn_f32(false, dtype, head_dim, t, b, max_blocks, s);
+    case LC_HEAD_ROPE:
+    case LC_HEAD_ROPE_BWD:
+    case LC_HEAD_GAIN:
+    case LC_COL_SUM: return launch_heads(cls, dtype, t, b, max_blocks, s);
+    case LC_ATTN_BWD_RULE: return launch_attn_f32(true, true, dtype, head_dim, t, b, max_blocks, s);
+    case LC_ATTN_RULE_F32: return launch_attn_f32(false, true, dtype, head_dim, t, b, max_blocks, s);
+    case LC_ATTN_BWD: return launch_attn_f32(true, false, dtype, head_dim, t, b, max_blocks, s);
+    case LC_ATTN_F32: return launch_attn_f32(false, false, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BF16:
       if (head_dim == 64) {
         hipLaunchKernelGGL(attn_bf16_kernel<64>, grid, wg, 4 * 64 * 64 * 2, s, t, b);

@@ -35,11 +35,76 @@ static bool same(const tn_tensor_desc& a, const tn_tensor_desc& b) {
   return a.dtype == b.dtype && a.rows == b.rows && a.cols == b.cols;
 }
 
+// Operands of a score rule, behind the `first` operands of an attention vertex: how many they are, and whether they fit.
+static int64_t rule_operands(const tn_op_params& p) { return (p.slopes ? 1 : 0) + (p.spans ? (int64_t)p.n_q_tiles : 0); }
+static tn_status validate_rule(const TaskGraph& g, const char* name, const tn_op_params& p, const tn_vid* in, int32_t first, int64_t hpg,
+                               bool finished) {
+  if (!(p.score_cap == 0.f || (p.score_cap >= 1e-6f && p.score_cap <= 1e6f))) return fail(TN_ERR_SHAPE, "%s: score_cap must be 0 or lie in 1e-6 .. 1e6", name);
+  if (!has_rule(p) && !finished) return TN_OK;
+  // caps and slopes are of scores that are scaled already, and the kernels count positions in 32 bits
+  if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(TN_ERR_SHAPE, "%s: a score rule and finished rows need a positive scale", name);
+  if (p.q_pos0 < 0 || p.k_pos0 < 0 || p.q_pos0 > (1 << 30) || p.k_pos0 > (1 << 30))
+    return fail(TN_ERR_SHAPE, "%s: with a score rule or finished rows q_pos0 and k_pos0 lie in 0 .. 2^30", name);
+  if (p.slopes) {
+    const tn_tensor_desc& d = g.v[in[first]].desc;
+    if (d.dtype != TN_F32 || d.rows != 1 || d.cols != hpg) return fail(TN_ERR_SHAPE, "%s: the slopes must be fp32 [1,%lld]", name, (long long)hpg);
+    ++first;
+  }
+  for (int r = 0; p.spans && r < p.n_q_tiles; ++r) {
+    const tn_tensor_desc& d = g.v[in[first + r]].desc;
+    if (d.dtype != TN_I32 || d.cols != 2 || d.rows != g.v[in[r * p.n_col_tiles]].desc.rows)
+      return fail(TN_ERR_SHAPE, "%s: the spans of Q row tile %d must be TN_I32 [rows, 2]", name, r);
+  }
+  return TN_OK;
+}
+
+static tn_status validate_head_rope(const TaskGraph& g, const tn_op_params& p, bool backward, const tn_vid* in, int32_t n_in,
+                                    const tn_tensor_desc& out) {
+  const char* name = backward ? "head_rope_bwd" : "head_rope";
+  const bool norm = p.norm != 0;
+  auto D = [&](int i) -> const tn_tensor_desc& { return g.v[in[i]].desc; };
+  if (backward && !norm) return fail(TN_ERR_SHAPE, "head_rope_bwd: needs norm (the gradient of a rotation alone is head_rope with mode 1)");
+  if (p.mode != 0 && p.mode != 1) return fail(TN_ERR_SHAPE, "%s: mode must be 0 or 1", name);
+  if (!backward && norm && p.mode) return fail(TN_ERR_SHAPE, "head_rope: norm does not go with the inverse rotation");
+  const int32_t x = backward ? 1 : 0, want = x + 1 + (norm ? 1 : 0) + (p.positions ? 1 : 0);
+  if (n_in != want) return fail(TN_ERR_SHAPE, "%s: needs %d operands", name, want);
+  const tn_tensor_desc& dx = D(x);
+  if (p.head_dim < 2 || (p.head_dim & 1) || p.head_dim > 1024 || dx.cols % p.head_dim)
+    return fail(TN_ERR_SHAPE, "%s: head_dim must be even and at most 1024, and the columns whole heads", name);
+  if (p.rotary_dim < 0 || (p.rotary_dim & 1) || p.rotary_dim > p.head_dim) return fail(TN_ERR_SHAPE, "%s: rotary_dim must be even and at most head_dim", name);
+  if (p.pos0 < 0 || !(p.rope_base > 0.f) || !std::isfinite(p.rope_base)) return fail(TN_ERR_SHAPE, "%s: pos0 must not be negative, rope_base positive", name);
+  if (!(p.rope_factor == 0.f || p.rope_factor >= 1.f) || !std::isfinite(p.rope_factor) || p.rope_len0 < 0)
+    return fail(TN_ERR_SHAPE, "%s: rope_factor must be 0 or at least 1, rope_len0 not negative", name);
+  if (p.rope_factor > 1.f && p.rope_len0 > 0 && (!(p.rope_low >= 0.f) || !(p.rope_high > p.rope_low) || !std::isfinite(p.rope_high)))
+    return fail(TN_ERR_SHAPE, "%s: rope_high must be above rope_low, and that not negative", name);
+  if (norm) {
+    if (!(p.eps >= 0.f) || !std::isfinite(p.eps)) return fail(TN_ERR_SHAPE, "%s: eps must not be negative", name);
+    if (D(x + 1).rows != 1 || D(x + 1).cols != p.head_dim || D(x + 1).dtype != dx.dtype)
+      return fail(TN_ERR_SHAPE, "%s: the gain must be [1, head_dim] of X's type", name);
+  }
+  if (p.positions && (D(n_in - 1).dtype != TN_I32 || D(n_in - 1).rows != dx.rows || D(n_in - 1).cols != 1))
+    return fail(TN_ERR_SHAPE, "%s: the positions must be TN_I32 [rows, 1]", name);
+  if (backward && !same(D(0), dx)) return fail(TN_ERR_SHAPE, "head_rope_bwd: dY must have X's shape and type");
+  if (backward && p.mode == 1) {
+    if (out.dtype != TN_F32 || out.rows != (dx.rows + 31) / 32 || out.cols != p.head_dim)
+      return fail(TN_ERR_SHAPE, "head_rope_bwd: mode 1 gives fp32 [ceil(rows / 32), head_dim]");
+  } else if (!same(dx, out)) {
+    return fail(TN_ERR_SHAPE, "%s: the output must have X's shape and type", name);
+  }
+  return TN_OK;
+}
+
 tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, const tn_vid* in,
                       int32_t n_in, const tn_tensor_desc& out) {
   auto D = [&](int i) -> const tn_tensor_desc& { return g.v[in[i]].desc; };
   if (out.rows <= 0 || out.cols <= 0 || (out.dtype != TN_F32 && out.dtype != TN_BF16))
     return fail(TN_ERR_SHAPE, "output tensor must be non-empty fp32 or bf16");
+  // integers are the positions of a rotation and the spans of a score rule, the last operands of these kinds
+  int64_t n_whole = 0;
+  if ((kind == TN_OP_HEAD_ROPE || kind == TN_OP_HEAD_ROPE_BWD) && p.positions) n_whole = 1;
+  if ((kind == TN_OP_ATTN_BLOCK || (kind == TN_OP_ATTN_BWD && p.mode != 4)) && p.spans) n_whole = std::max(0, p.n_q_tiles);
+  for (int64_t i = 0; i < n_in - n_whole; ++i)
+    if (D((int)i).dtype == TN_I32) return fail(TN_ERR_SHAPE, "operand %lld of vertex kind %d must not be integers", (long long)i, kind);
   switch (kind) {
     case TN_OP_GEMM: {
       if (p.mode < 0 || p.mode > 2) return fail(TN_ERR_SHAPE, "gemm: mode must be 0, 1 or 2");
@@ -92,8 +157,9 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
     }
     case TN_OP_ATTN_BLOCK: {
       int nq = p.n_q_tiles, nkv = p.n_kv_tiles, nc = p.n_col_tiles;
-      if (nq < 1 || nkv < 1 || nc < 1 || n_in != (nq + 2 * nkv) * nc || p.head_dim < 1)
-        return fail(TN_ERR_SHAPE, "attn_block: needs (n_q_tiles + 2 n_kv_tiles) * n_col_tiles operands");
+      if (nq < 1 || nkv < 1 || nc < 1 || n_in != ((int64_t)nq + 2ll * nkv) * nc + rule_operands(p) || p.head_dim < 1)
+        return fail(TN_ERR_SHAPE, "attn_block: needs (n_q_tiles + 2 n_kv_tiles) * n_col_tiles operands, plus those of its score rule");
+      if (p.finish != 0 && p.finish != 1) return fail(TN_ERR_SHAPE, "attn_block: finish must be 0 or 1");
       int64_t gw = 0, qrows = 0;
       for (int c = 0; c < nc; ++c) gw += D(c).cols;
       if (gw % p.head_dim) return fail(TN_ERR_SHAPE, "attn_block: columns are not whole heads");
@@ -114,6 +180,12 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
             return fail(TN_ERR_SHAPE, "attn_block: K/V tile (%d,%d) does not fit the grid", r, c);
         }
       int64_t hpg = gw / p.head_dim;
+      if (const tn_status st = validate_rule(g, "attn_block", p, in, (nq + 2 * nkv) * nc, hpg, p.finish != 0); st != TN_OK) return st;
+      if (p.finish) {
+        if (out.dtype != dt || out.rows != qrows || out.cols != gw)
+          return fail(TN_ERR_SHAPE, "attn_block: finished rows are [%lld,%lld] of the operands' type", (long long)qrows, (long long)gw);
+        return TN_OK;
+      }
       if (out.dtype != TN_F32 || out.rows != qrows || out.cols != gw + 2 * hpg)
         return fail(TN_ERR_SHAPE, "attn_block: output must be fp32 [%lld,%lld]", (long long)qrows,
                     (long long)(gw + 2 * hpg));
@@ -125,6 +197,12 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
       for (int i = 0; i < n_in; ++i)
         if (D(i).dtype != TN_F32 || D(i).cols != gw + 2 * p.hpg || D(i).rows != D(0).rows)
           return fail(TN_ERR_SHAPE, "attn_combine: operand %d is not a partial of this group", i);
+      if (p.finish < 0 || p.finish > 2) return fail(TN_ERR_SHAPE, "attn_combine: finish must be 0, 1 or 2");
+      if (p.finish == 2) {
+        if (out.dtype != TN_F32 || out.cols != p.hpg || p.row0 < 0 || p.col0 != 0 || (int64_t)p.row0 + out.rows > D(0).rows)
+          return fail(TN_ERR_SHAPE, "attn_combine: finish 2 gives fp32 [rows, hpg] of rows inside the block");
+        return TN_OK;
+      }
       if (p.row0 < 0 || p.col0 < 0 || p.row0 + out.rows > D(0).rows || p.col0 + out.cols > gw)
         return fail(TN_ERR_SHAPE, "attn_combine: output window leaves the block");
       return TN_OK;
@@ -184,13 +262,44 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
       if (n_in != 1 || D(0).rows != out.cols || D(0).cols != out.rows || D(0).dtype != out.dtype)
         return fail(TN_ERR_SHAPE, "transpose: one operand [cols, rows] of the output's type");
       return TN_OK;
+    case TN_OP_HEAD_ROPE:
+    case TN_OP_HEAD_ROPE_BWD:
+      return validate_head_rope(g, p, kind == TN_OP_HEAD_ROPE_BWD, in, n_in, out);
+    case TN_OP_COL_SUM:
+      if (out.dtype != TN_F32 || out.rows != 1) return fail(TN_ERR_SHAPE, "col_sum: the output is fp32 [1, cols]");
+      for (int i = 0; i < n_in; ++i)
+        if (D(i).dtype != TN_F32 || D(i).cols != out.cols) return fail(TN_ERR_SHAPE, "col_sum: operand %d is not fp32 of the output's columns", i);
+      return TN_OK;
     case TN_OP_ATTN_BWD: {
       const int nq = p.n_q_tiles, nkv = p.n_kv_tiles, nc = p.n_col_tiles;
+      if (p.mode == 4) {  // statistics from O, dO and the log-sum-exp
+        if (nq < 1 || nc < 1 || p.head_dim < 1 || n_in != 2ll * nq * nc + nq)
+          return fail(TN_ERR_SHAPE, "attn_bwd: mode 4 needs 2 n_q_tiles * n_col_tiles operands and n_q_tiles log-sum-exps");
+        int64_t gw = 0, qrows = 0;
+        for (int c = 0; c < nc; ++c) gw += D(c).cols;
+        if (gw % p.head_dim) return fail(TN_ERR_SHAPE, "attn_bwd: columns are not whole heads");
+        for (int r = 0; r < nq; ++r) {
+          qrows += D(r * nc).rows;
+          for (int c = 0; c < nc; ++c) {
+            const auto& o = D(r * nc + c);
+            if (o.rows != D(r * nc).rows || o.cols != D(c).cols || o.dtype != D(0).dtype || !same(o, D((nq + r) * nc + c)))
+              return fail(TN_ERR_SHAPE, "attn_bwd: O / dO tile (%d,%d) does not fit the grid", r, c);
+          }
+          const auto& l = D(2 * nq * nc + r);
+          if (l.dtype != TN_F32 || l.rows != D(r * nc).rows || l.cols != gw / p.head_dim)
+            return fail(TN_ERR_SHAPE, "attn_bwd: the log-sum-exp of Q row tile %d must be fp32 [rows, hpg]", r);
+        }
+        if (out.dtype != TN_F32 || out.rows != qrows || out.cols != 2 * (gw / p.head_dim))
+          return fail(TN_ERR_SHAPE, "attn_bwd: output shape does not fit mode 4");
+        return TN_OK;
+      }
+      if (has_rule(p) && (p.mode < 1 || p.trans_a))
+        return fail(TN_ERR_SHAPE, "attn_bwd: a score rule goes with modes 1 to 3 (statistics: mode 4) and without transposed grids");
       if (nq < 1 || nkv < 1 || nc < 1 || p.head_dim < 1 || p.mode < 0 || p.mode > 3 ||
           (p.trans_a && (p.mode == 0 || p.v_trans)) ||
-          n_in != (2 * nq + 2 * nkv) * nc + (p.mode ? nq : 0) + (p.trans_a ? (p.mode == 1 ? nkv : nq) * nc : 0))
+          n_in != 2 * ((int64_t)nq + nkv) * nc + (p.mode ? nq : 0) + (p.trans_a ? (int64_t)(p.mode == 1 ? nkv : nq) * nc : 0) + rule_operands(p))
         return fail(TN_ERR_SHAPE, "attn_bwd: needs (2 n_q_tiles + 2 n_kv_tiles) * n_col_tiles operands, plus n_q_tiles "
-                                  "statistics unless mode is 0, plus the transposed grid if trans_a is set");
+                                  "statistics unless mode is 0, plus the transposed grid if trans_a is set, plus those of its score rule");
       int64_t gw = 0, qrows = 0, kvrows = 0;
       for (int c = 0; c < nc; ++c) gw += D(c).cols;
       if (gw % p.head_dim) return fail(TN_ERR_SHAPE, "attn_bwd: columns are not whole heads");
@@ -216,6 +325,7 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
             return fail(TN_ERR_SHAPE, "attn_bwd: K/V tile (%d,%d) does not fit the grid", r, c);
         }
       }
+      if (const tn_status st = validate_rule(g, "attn_bwd", p, in, s0 + nq, hpg, false); st != TN_OK) return st;
       if (p.trans_a) {
         const int t0 = s0 + nq, src0 = p.mode == 1 ? nq * nc : p.mode == 2 ? 0 : d0, cnt = (p.mode == 1 ? nkv : nq) * nc;
         for (int i = 0; i < cnt; ++i) {
@@ -410,8 +520,8 @@ void tn_taskgraph_destroy(tn_taskgraph* tg) { delete tg; }
 
 tn_status tn_taskgraph_add_input(tn_taskgraph* tg, const tn_tensor_desc* desc, int32_t residency, tn_vid* out) {
   if (!tg || !desc || !out) return fail(TN_ERR_INVALID, "NULL argument");
-  if (desc->rows <= 0 || desc->cols <= 0 || (desc->dtype != TN_F32 && desc->dtype != TN_BF16))
-    return fail(TN_ERR_SHAPE, "input tensor must be non-empty fp32 or bf16");
+  if (desc->rows <= 0 || desc->cols <= 0 || (desc->dtype != TN_F32 && desc->dtype != TN_BF16 && desc->dtype != TN_I32))
+    return fail(TN_ERR_SHAPE, "input tensor must be non-empty fp32, bf16 or 32-bit integers");
   if (residency != TN_HOST && residency != TN_DEVICE) return fail(TN_ERR_INVALID, "bad residency");
   Vertex v;
   v.kind = TN_OP_INPUT;

@@ -425,7 +425,9 @@ tn_status build_tables(tn_executor& ex) {
         aux.insert(aux.end(), {tq, tk, tc, q_rows, kv_rows});
         if (has_rule(x.p) || x.p.finish) {
           add_rule(x.p, (nq + 2 * nkv) * nc);
-          vi.cls = LC_ATTN_RULE_F32;
+          // the bf16 kernel wants plain V tiles, whole heads inside one column tile and 64-key chunks inside one row tile
+          vi.cls = (d.dtype == TN_BF16 && !x.p.v_trans && tc % hd == 0 && (nkv == 1 || tk % 64 == 0))
+                       ? (int8_t)(LC_ATTN_RULE_BF16 + (x.p.score_cap > 0.f ? kRuleHasCap : 0) + (x.p.slopes ? kRuleHasSlopes : 0)) : (int8_t)LC_ATTN_RULE_F32;
           vi.head_dim = (int16_t)hd;
           vi.flops = 4.0 * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
           vi.bytes = (q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
@@ -691,6 +693,10 @@ int family_of(int cls) {
     case LC_ATTN_BWD_BF16_DK:
     case LC_ATTN_BWD_BF16_DV:
     case LC_ATTN_RULE_F32:
+    case LC_ATTN_RULE_BF16:
+    case LC_ATTN_RULE_BF16 + 1:
+    case LC_ATTN_RULE_BF16 + 2:
+    case LC_ATTN_RULE_BF16_LAST:
     case LC_ATTN_BWD_RULE: return 1;
     default: return 2;
   }

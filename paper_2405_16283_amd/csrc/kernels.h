@@ -87,6 +87,8 @@ enum LaunchClass {
   LC_COL_SUM,
   LC_ATTN_RULE_F32,  // attention with a score rule or finished rows, fp32 products
   LC_ATTN_BWD_RULE,  // its gradients, fp32 products
+  LC_ATTN_RULE_BF16, // attention with a score rule or finished rows, bf16 products: plus kRuleHasCap and kRuleHasSlopes
+  LC_ATTN_RULE_BF16_LAST = LC_ATTN_RULE_BF16 + 3,
   LC_ATTN_STATS,     // their statistics from O, dO and the log-sum-exp
   LC_ATTN_JOIN,      // combine with finish 1
   LC_ATTN_LSE,       // combine with finish 2
@@ -201,6 +203,11 @@ hipError_t launch_gemm_rows(int dtype, const DeviceTables& t, uint32_t base, con
 // Auxiliary integers of attention vertices: rows per Q tile, rows per K/V tile, columns per tile, q rows, kv rows; those with a score
 // rule or finished rows have these behind them.
 enum { kRuleCap = 5, kRuleSlopes, kRuleSpans, kRuleFinish, kRuleAux };  // bits of score_cap; operand of the slopes and of the first spans, or -1
+
+enum { kRuleHasCap = 1, kRuleHasSlopes = 2 };  // kernels of their own
+// LC_ATTN_RULE_BF16 and the three behind it: attn_rule.hip.
+int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux);
+hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
 // LC_HEAD_ROPE to LC_COL_SUM: heads.hip.  Auxiliary integers of the first three (of LC_COL_SUM: rows per operand):
 enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadAux };

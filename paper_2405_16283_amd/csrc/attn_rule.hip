@@ -1,4 +1,4 @@
-// Attention by a score rule (turnip.h: score_cap, slopes, spans) with bf16 products on the matrix cores: forward.
+// Attention by a score rule (turnip.h: score_cap, slopes, spans) with bf16 products on the matrix cores, forward and reverse.
 //
 // One workgroup = one head x 128 query rows; each of its 4 wavefronts owns 32 of them, two workgroups share a compute unit.  Per
 // 32 keys a wavefront forms the transposed scores S^T = K Q^T (MFMA 32x32x16), so that a lane owns one query -- its span, position and
@@ -270,6 +270,290 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
   }
 }
 
+// Reverse pass, the same way round: a lane owns one row of its own side -- a query for dQ (mode 1), a key for dK (2) and dV (3) -- and
+// the other side comes in chunks of 64 rows.  Per 32 of them S^T is formed again, with dP^T = V dO^T (or its transpose) beside it, and
+// the gradient is summed transposed, dQ^T += K^T dS^T, dK^T += Q^T dS, dV^T += dO^T P, its left operand read transposed out of the
+// chunk that is there already: no transposed tensors.
+//
+// What is subtracted goes in as the products' starting value: S starts at -lse / scale, so that the weight is exp2(scale2 * S)
+// (with a cap the exponent is formed from 1 / (1 + exp(2 z / cap)), whose y - y^2 is a quarter of the cap's derivative), and dP at
+// -D.  Weights and their gradients enter the second product as single bf16, as in the forward pass.
+constexpr int kBwdStats = 4 * kRuleKeys * 4;  // of a stage's queries (modes 2, 3): -lse / scale or cap2 - lse2, -D, first key seen, the one behind the last
+constexpr int attn_rule_bwd_lds(int hd) { return 2 * (2 * kRuleKeys * hd * 2 + kBwdStats); }
+
+template <int HD, int MODE, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  constexpr bool OWN_Q = MODE == 1;
+  constexpr int CH = kRuleKeys, CPR = HD / 8, ABYTES = CH * HD * 2, STAGE = 2 * ABYTES + kBwdStats;
+  constexpr int NLD = CH * CPR / 256;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int* ax = t.aux + d.aux0;
+  const int tq = ax[0], tk = ax[1], tc = ax[2], q_rows = ax[3], kv_rows = ax[4];
+  const int nc = d.p.n_col_tiles, gw = nc * tc, hpg = gw / HD, nq = d.p.n_q_tiles, nkv = d.p.n_kv_tiles;
+  void* const* Qt = t.ptrs + d.ptr0;
+  void* const* Kt = Qt + nq * nc;
+  void* const* Vt = Kt + nkv * nc;
+  void* const* Dt = Vt + nkv * nc;  // dO tiles
+  void* const* St = Dt + nq * nc;   // statistics per Q row tile
+  const int my_rows = OWN_Q ? q_rows : kv_rows, o_rows = OWN_Q ? kv_rows : q_rows, my_trows = OWN_Q ? tq : tk, o_trows = OWN_Q ? tk : tq;
+  int h, rb;
+  {
+    const int blocks = (my_rows + kRuleRows - 1) / kRuleRows;
+    head_and_block(blockIdx.x, hpg, blocks, h, rb);
+    if (OWN_Q) rb = blocks - 1 - rb;  // late queries see most; early keys are seen most
+  }
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, g = lane >> 5;
+  const int row0 = rb * kRuleRows + w * 32, row = row0 + l32;
+  const bool exists = row < my_rows;
+  const Rule rule(t, d);
+  auto stat = [&](int r, int which) -> float {
+    const int rt = r / tq;
+    return ((const float*)St[rt])[(size_t)(r - rt * tq) * (2 * hpg) + which * hpg + h];
+  };
+  const float scale2 = d.p.scale * kLog2e, inv_scale = 1.f / d.p.scale;
+  const float cap2 = rule.cap * kLog2e, into_tanh = 2.f * kLog2e * d.p.scale * rule.inv_cap;
+  const float slope2 = SLOPES ? rule.slope(h) * kLog2e : 0.f;
+  // what is added to a score: in the units of the product, or of the exponent
+  auto start = [&](float lse) { return CAP || SLOPES ? (CAP ? cap2 : 0.f) - lse * kLog2e : -lse * inv_scale; };
+
+  int lo = 0, hi = 0;                                           // mode 1: the keys this lane's query sees
+  int w_begin = 0, w_end = 0, all_lo = 0, all_hi = 0;           // mode 1: of the wavefront
+  const int key0 = row0, key1 = min(row0 + 32, kv_rows);        // modes 2, 3: the wavefront's keys
+  int begin, end;                                               // rows of the other side that the workgroup has to do with
+  {
+    int v0 = INT_MAX, v1 = INT_MAX;  // minima of the first and of minus the one behind the last
+    if (OWN_Q) {
+      if (exists) rule.visible(row, lo, hi);
+      w_begin = wave_min(lo < hi ? lo : INT_MAX);
+      w_end = -wave_min(-hi);
+      all_lo = -wave_min(exists ? -lo : INT_MAX);
+      all_hi = wave_min(exists ? hi : INT_MAX);
+      v0 = w_begin;
+      v1 = -w_end;
+    } else {
+      const int k0 = rb * kRuleRows, k1 = min(k0 + kRuleRows, kv_rows);
+      const int first = rule.causal ? max(0, rule.k_pos0 + k0 - rule.q_pos0) : 0;
+      if (rule.spans) {
+#pragma unroll 8
+        for (int q = first + threadIdx.x; q < q_rows; q += 256) {
+          int ql, qh;
+          rule.visible(q, ql, qh);
+          if (ql < k1 && qh > k0) {
+            v0 = min(v0, q);
+            v1 = min(v1, -q - 1);
+          }
+        }
+        v0 = wave_min(v0);
+        v1 = wave_min(v1);
+      } else if (first < q_rows) {
+        v0 = first;
+        v1 = -q_rows;
+      }
+    }
+    int* const shared = (int*)lds;
+    if (lane == 0) {
+      shared[2 * w] = v0;
+      shared[2 * w + 1] = v1;
+    }
+    __syncthreads();
+    begin = min(min(shared[0], shared[2]), min(shared[4], shared[6]));
+    end = -min(min(shared[1], shared[3]), min(shared[5], shared[7]));
+    begin = __builtin_amdgcn_readfirstlane(begin < end ? begin & ~(CH - 1) : end);
+    end = __builtin_amdgcn_readfirstlane(end);
+    __syncthreads();
+  }
+
+  // this lane's own row: Q and dO, or K and V (dV needs no V)
+  bf16x8 mine[HD / 16], mine2[HD / 16];
+  {
+    const int r = min(row, my_rows - 1);
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) {
+      mine[s] = *(const bf16x8*)tile_elem<bf16_t>(OWN_Q ? Qt : Kt, nc, my_trows, tc, r, h * HD + s * 16 + g * 8);
+      if (MODE != 3) mine2[s] = *(const bf16x8*)tile_elem<bf16_t>(OWN_Q ? Dt : Vt, nc, my_trows, tc, r, h * HD + s * 16 + g * 8);
+    }
+  }
+  const float my_start = OWN_Q ? start(stat(min(row, q_rows - 1), 0)) : 0.f, my_D = OWN_Q ? -stat(min(row, q_rows - 1), 1) : 0.f;
+  f32x16 acc[HD / 32];
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+
+  // the other side's chunks (layouts: see the forward kernel): K | V, or Q | dO, then the statistics
+  void* const* gridA = OWN_Q ? Kt : Qt;
+  void* const* gridB = OWN_Q ? Vt : Dt;
+  const uint32_t lds0 = (uint32_t)(size_t)(lptr_t)lds;
+  const int ct = (h * HD) / tc, cin0 = (h * HD) % tc;
+  int rt = -1, trows = 0;
+  const bf16_t* At = nullptr;
+  const bf16_t* Bt = nullptr;
+  auto issue = [&](int o0, int stg) {
+    const int nrt = o0 / o_trows;
+    if (nrt != rt) {
+      rt = nrt;
+      At = (const bf16_t*)sload_ptr((const void* const*)(gridA + rt * nc + ct));
+      Bt = (const bf16_t*)sload_ptr((const void* const*)(gridB + rt * nc + ct));
+      trows = min(o_trows, o_rows - rt * o_trows);
+    }
+    const int in = o0 - rt * o_trows;
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + stg * STAGE + w * 1024);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) {
+      const int p = i * 256 + threadIdx.x, r = p / CPR;
+      const size_t at = (size_t)min(in + r, trows - 1) * tc + (cin0 + ((p % CPR) ^ swizzle<HD>(r)) * 8);  // rows past the end: one that exists, hidden below
+      load_lds(At + at, dst + i * 4096);
+      load_lds(Bt + at, dst + ABYTES + i * 4096);
+    }
+  };
+  // the statistics of a chunk's queries travel through registers of its first CH threads
+  float s_start = 0.f, s_D = 0.f;
+  int s_lo = 0, s_hi = 0;
+  auto load_stats = [&](int o0) {
+    if (OWN_Q || threadIdx.x >= CH) return;
+    const int q = o0 + threadIdx.x, qc = min(q, q_rows - 1);
+    s_start = start(stat(qc, 0));
+    s_D = -stat(qc, 1);
+    s_lo = s_hi = 0;
+    if (q < q_rows) rule.visible(q, s_lo, s_hi);
+  };
+
+  const int a_ = l32 >> 3, b_ = l32 & 3, g_ = (l32 >> 2) & 1;
+  const int perm = 16 * (a_ >> 1) + 8 * g_ + 4 * (a_ & 1) + b_;
+  const int k_at = perm * (HD * 2), k_sw = swizzle<HD>(perm);
+  const int v_row = 8 * g + ((lane & 15) >> 2), v_piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), v_in = (lane & 1) * 8;
+  const float from_me = (float)(rule.q_pos0 - rule.k_pos0 + (OWN_Q ? row : -row));  // query position - key position, less the other side's index
+
+  if (begin < end) {
+    issue(begin, 0);
+    load_stats(begin);
+  }
+  int stg = 0;
+  for (int o0 = begin; o0 < end; o0 += CH, stg ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this chunk and its statistics have arrived
+    char* const stage = lds + stg * STAGE;
+    float* const st = (float*)(stage + 2 * ABYTES);
+    if (!OWN_Q && threadIdx.x < CH) {
+      st[threadIdx.x] = s_start;
+      st[CH + threadIdx.x] = s_D;
+      ((int*)st)[2 * CH + threadIdx.x] = s_lo;
+      ((int*)st)[3 * CH + threadIdx.x] = s_hi;
+    }
+    __syncthreads();  // ... for everybody, and everybody is done with the other stage
+    if (o0 + CH < end) {
+      issue(o0 + CH, stg ^ 1);
+      load_stats(o0 + CH);
+    }
+#pragma unroll 1
+    for (int sub = 0; sub < 2; ++sub) {
+      const int os = o0 + sub * 32;
+      bool all_see;
+      if (OWN_Q) {
+        if (os + 32 <= w_begin || os >= w_end) continue;
+        all_see = os >= all_lo && os + 32 <= all_hi;
+      } else {
+        const int ql = ((const int*)st)[2 * CH + sub * 32 + l32], qh = ((const int*)st)[3 * CH + sub * 32 + l32];
+        if (!__any(ql < key1 && qh > key0)) continue;
+        all_see = __all(ql <= key0 && qh >= row0 + 32);
+      }
+      const char* ra = stage + sub * 32 * (HD * 2) + k_at;
+      f32x16 s, dp;
+      // register r: row os + 16 (r >> 3) + 8 g + (r & 7) of the other side
+      float starts[16];
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        f32x4 v = {my_start, my_start, my_start, my_start}, vd = {my_D, my_D, my_D, my_D};
+        if (!OWN_Q) {
+          const int at = sub * 32 + 16 * (r >> 3) + 8 * g + (r & 7);
+          v = *(const f32x4*)(st + at);
+          if (MODE == 2) vd = *(const f32x4*)(st + CH + at);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          starts[r + e] = v[e];
+          s[r + e] = CAP || SLOPES ? 0.f : v[e];
+          dp[r + e] = vd[e];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) {
+        const int at = ((2 * j + g) ^ k_sw) * 16;
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(ra + at), mine[j], s, 0, 0, 0);
+        if (MODE != 3) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(ra + ABYTES + at), mine2[j], dp, 0, 0, 0);
+      }
+      const float base = from_me + (OWN_Q ? -(float)(os + 8 * g) : (float)(os + 8 * g));
+      float pr[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int c = 16 * (r >> 3) + (r & 7);
+        float x, y = 0.f;
+        if (CAP) {
+          y = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * into_tanh) + 1.f);
+          x = __builtin_fmaf(-2.f * cap2, y, starts[r]);
+        } else {
+          x = SLOPES ? __builtin_fmaf(s[r], scale2, starts[r]) : s[r] * scale2;
+        }
+        if (SLOPES) x = __builtin_fmaf(-slope2, fabsf(base + (OWN_Q ? -(float)c : (float)c)), x);
+        float p = __builtin_amdgcn_exp2f(x);
+        if (MODE != 3) p *= dp[r];
+        if (CAP && MODE != 3) p *= __builtin_fmaf(-y, y, y);
+        pr[r] = p;
+      }
+      if (!all_see) {
+        if (OWN_Q) {
+          const int first = lo - os - 8 * g;
+          const uint32_t len = hi - lo;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) pr[r] = (uint32_t)(16 * (r >> 3) + (r & 7) - first) < len ? pr[r] : 0.f;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int at = sub * 32 + 16 * (r >> 3) + 8 * g + (r & 7);
+            pr[r] = row >= ((const int*)st)[2 * CH + at] && row < ((const int*)st)[3 * CH + at] ? pr[r] : 0.f;
+          }
+        }
+      }
+      union { uint32_t u[4]; bf16x8 v; } p[2];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) p[r >> 3].u[(r & 7) >> 1] = f2bf2(pr[r], pr[r + 1]);
+      const char* const tb = stage + (MODE == 3 ? ABYTES : 0);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < HD / 32; ++i) {
+          union { s16x4 h[2]; bf16x8 v; } a;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = ks * 16 + 4 * e + v_row;  // (sub * 32 leaves the swizzle alone)
+            a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(tb + sub * 32 * (HD * 2) + r * (HD * 2) + ((i * 4 + v_piece) ^ swizzle<HD>(r)) * 16 + v_in));
+          }
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[ks].v, acc[i], 0, 0, 0);
+        }
+    }
+  }
+  // a weight of zero times an infinity or NaN of a row that does not matter to this one: such rows are formed again
+  float z = 0.f;
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = fmaf(acc[i][r], 0.f, z);
+  if (__builtin_expect(__any(exists && !(z == 0.f)), 0)) {
+    const Side<bf16_t, HD> Q(Qt, nc, tq, tc, q_rows, h), K(Kt, nc, tk, tc, kv_rows, h), V(Vt, nc, tk, tc, kv_rows, h), D(Dt, nc, tq, tc, q_rows, h);
+    return attn_bwd_by_rows<bf16_t, HD, MODE, true>(t, d, Q, K, V, D, h, gw, row0, row0 + 32, lane >> 4, 4, stat);
+  }
+  if (!exists) return;
+  const float oscale = MODE == 3 ? 1.f : CAP ? 4.f * d.p.scale : d.p.scale;
+  bf16_t* out = (bf16_t*)d.out + (size_t)row * gw + h * HD + 4 * g;
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+      *(uint2*)(out + i * 32 + 8 * a) =
+          make_uint2(f2bf2(acc[i][4 * a] * oscale, acc[i][4 * a + 1] * oscale), f2bf2(acc[i][4 * a + 2] * oscale, acc[i][4 * a + 3] * oscale));
+}
+
 template <auto kernel>
 hipError_t launch(int threads, int lds, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
@@ -290,14 +574,36 @@ hipError_t launch_forward(int rule, const DeviceTables& t, const Batch& b, int32
   }
 }
 
+template <int HD, int MODE>
+hipError_t launch_reverse(int rule, const DeviceTables& t, const Batch& b, int32_t n, hipStream_t s) {
+  constexpr int lds = attn_rule_bwd_lds(HD);
+  switch (rule) {
+    case 0: return launch<attn_rule_bwd_kernel<HD, MODE, false, false>>(256, lds, t, b, n, s);
+    case kRuleHasCap: return launch<attn_rule_bwd_kernel<HD, MODE, true, false>>(256, lds, t, b, n, s);
+    case kRuleHasSlopes: return launch<attn_rule_bwd_kernel<HD, MODE, false, true>>(256, lds, t, b, n, s);
+    default: return launch<attn_rule_bwd_kernel<HD, MODE, true, true>>(256, lds, t, b, n, s);
+  }
+}
+template <int HD>
+hipError_t launch_reverse(int mode, int rule, const DeviceTables& t, const Batch& b, int32_t n, hipStream_t s) {
+  return mode == 1 ? launch_reverse<HD, 1>(rule, t, b, n, s) : mode == 2 ? launch_reverse<HD, 2>(rule, t, b, n, s) : launch_reverse<HD, 3>(rule, t, b, n, s);
+}
+
 }  // namespace
 
 int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   const int32_t* ax = aux + d.aux0;
-  return d.p.n_col_tiles * ax[2] / d.p.head_dim * ((ax[3] + kRuleRows - 1) / kRuleRows);
+  const int rows = cls >= LC_ATTN_BWD_RULE_BF16 && d.p.mode != 1 ? ax[4] : ax[3];  // keys for dK and dV, else queries
+  return d.p.n_col_tiles * ax[2] / d.p.head_dim * ((rows + kRuleRows - 1) / kRuleRows);
 }
 
 hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+  if (cls >= LC_ATTN_BWD_RULE_BF16) {
+    const int mode = 1 + (cls - LC_ATTN_BWD_RULE_BF16) / 4, rule = (cls - LC_ATTN_BWD_RULE_BF16) % 4;
+    if (head_dim == 64) return launch_reverse<64>(mode, rule, t, b, max_blocks, s);
+    if (head_dim == 128) return launch_reverse<128>(mode, rule, t, b, max_blocks, s);
+    return hipErrorInvalidValue;
+  }
   if (head_dim == 64) return launch_forward<64>(cls - LC_ATTN_RULE_BF16, t, b, max_blocks, s);
   if (head_dim == 128) return launch_forward<128>(cls - LC_ATTN_RULE_BF16, t, b, max_blocks, s);
   return hipErrorInvalidValue;

@@ -247,6 +247,8 @@ int gemm_form(int64_t n256, int64_t n128) {
   return 0.6 * c128 < c256 ? LC_GEMM_BF16_PAIRED : LC_GEMM_BF16;
 }
 
+int rule_kernel(const tn_op_params& p) { return (p.score_cap > 0.f ? kRuleHasCap : 0) + (p.slopes ? kRuleHasSlopes : 0); }
+
 // the table pointers for a copy of the image that starts at `base`
 DeviceTables tables_at(const tn_executor& ex, const char* base) {
   return {(const OpDesc*)(base + ex.image_off[0]), (void* const*)(base + ex.image_off[1]),
@@ -427,7 +429,7 @@ tn_status build_tables(tn_executor& ex) {
           add_rule(x.p, (nq + 2 * nkv) * nc);
           // the bf16 kernel wants plain V tiles, whole heads inside one column tile and 64-key chunks inside one row tile
           vi.cls = (d.dtype == TN_BF16 && !x.p.v_trans && tc % hd == 0 && (nkv == 1 || tk % 64 == 0))
-                       ? (int8_t)(LC_ATTN_RULE_BF16 + (x.p.score_cap > 0.f ? kRuleHasCap : 0) + (x.p.slopes ? kRuleHasSlopes : 0)) : (int8_t)LC_ATTN_RULE_F32;
+                       ? (int8_t)(LC_ATTN_RULE_BF16 + rule_kernel(x.p)) : (int8_t)LC_ATTN_RULE_F32;
           vi.head_dim = (int16_t)hd;
           vi.flops = 4.0 * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
           vi.bytes = (q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
@@ -524,7 +526,9 @@ tn_status build_tables(tn_executor& ex) {
         aux.insert(aux.end(), {tq, tk, tc, q_rows, kv_rows});
         if (has_rule(x.p)) {
           add_rule(x.p, 2 * (nq + nkv) * nc + nq);
-          vi.cls = LC_ATTN_BWD_RULE;
+          // the bf16 kernels want plain V tiles, whole heads inside one column tile and 64-row chunks of the other side inside one row tile
+          vi.cls = (d.dtype == TN_BF16 && !x.p.v_trans && tc % hd == 0 && (x.p.mode == 1 ? nkv == 1 || tk % 64 == 0 : nq == 1 || tq % 64 == 0))
+                       ? (int8_t)(LC_ATTN_BWD_RULE_BF16 + 4 * (x.p.mode - 1) + rule_kernel(x.p)) : (int8_t)LC_ATTN_BWD_RULE;
           vi.head_dim = (int16_t)hd;
           vi.flops = (x.p.mode == 3 ? 4.0 : 6.0) * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
           vi.bytes = (2.0 * q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
@@ -693,12 +697,8 @@ int family_of(int cls) {
     case LC_ATTN_BWD_BF16_DK:
     case LC_ATTN_BWD_BF16_DV:
     case LC_ATTN_RULE_F32:
-    case LC_ATTN_RULE_BF16:
-    case LC_ATTN_RULE_BF16 + 1:
-    case LC_ATTN_RULE_BF16 + 2:
-    case LC_ATTN_RULE_BF16_LAST:
     case LC_ATTN_BWD_RULE: return 1;
-    default: return 2;
+    default: return is_attn_rule_bf16(cls) ? 1 : 2;
   }
 }
 

@@ -89,6 +89,8 @@ enum LaunchClass {
   LC_ATTN_BWD_RULE,  // its gradients, fp32 products
   LC_ATTN_RULE_BF16, // attention with a score rule or finished rows, bf16 products: plus kRuleHasCap and kRuleHasSlopes
   LC_ATTN_RULE_BF16_LAST = LC_ATTN_RULE_BF16 + 3,
+  LC_ATTN_BWD_RULE_BF16, // its gradients: plus 4 for dK, 8 for dV, and the same
+  LC_ATTN_BWD_RULE_BF16_LAST = LC_ATTN_BWD_RULE_BF16 + 11,
   LC_ATTN_STATS,     // their statistics from O, dO and the log-sum-exp
   LC_ATTN_JOIN,      // combine with finish 1
   LC_ATTN_LSE,       // combine with finish 2
@@ -205,7 +207,8 @@ hipError_t launch_gemm_rows(int dtype, const DeviceTables& t, uint32_t base, con
 enum { kRuleCap = 5, kRuleSlopes, kRuleSpans, kRuleFinish, kRuleAux };  // bits of score_cap; operand of the slopes and of the first spans, or -1
 
 enum { kRuleHasCap = 1, kRuleHasSlopes = 2 };  // kernels of their own
-// LC_ATTN_RULE_BF16 and the three behind it: attn_rule.hip.
+// LC_ATTN_RULE_BF16 to LC_ATTN_BWD_RULE_BF16_LAST: attn_rule.hip.
+inline bool is_attn_rule_bf16(int cls) { return cls >= LC_ATTN_RULE_BF16 && cls <= LC_ATTN_BWD_RULE_BF16_LAST; }
 int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux);
 hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 

@@ -1307,6 +1307,7 @@ __global__ void __launch_bounds__(kDeviceCopyThreads) device_copy_kernel(CopyBat
 static inline int32_t cdiv(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
 int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
+  if (is_attn_rule_bf16(cls)) return attn_rule_blocks(cls, d, aux);
   switch (cls) {
     case LC_GEMM_F32:
     case LC_GEMM_BF16_SMALL: return cdiv(d.rows, kGemmSmallTile) * cdiv(d.cols, kGemmSmallTile);
@@ -1321,10 +1322,6 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
     case LC_HEAD_ROPE_BWD:
     case LC_HEAD_GAIN:
     case LC_COL_SUM: return head_blocks(cls, d, aux);
-    case LC_ATTN_RULE_BF16:
-    case LC_ATTN_RULE_BF16 + 1:
-    case LC_ATTN_RULE_BF16 + 2:
-    case LC_ATTN_RULE_BF16_LAST: return attn_rule_blocks(cls, d, aux);
     case LC_ATTN_STATS: return cdiv((int64_t)d.rows * (d.p.n_col_tiles * aux[d.aux0 + 2] / d.p.head_dim), 16);
     case LC_ATTN_LSE: return cdiv((int64_t)d.rows * d.cols, 256);
     case LC_ATTN_RULE_F32:
@@ -1408,6 +1405,7 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
   if (b.n <= 0 || max_blocks <= 0) return hipSuccess;
   const dim3 grid((unsigned)max_blocks, (unsigned)b.n), wg(256);
   const bool bf = dtype == TN_BF16;
+  if (is_attn_rule_bf16(cls)) return launch_attn_rule(cls, head_dim, t, b, max_blocks, s);
 #define TN_LAUNCH_T(kernel)                                                     \
   do {                                                                          \
     if (bf) hipLaunchKernelGGL(kernel<bf16_t>, grid, wg, 0, s, t, b);           \
@@ -1468,10 +1466,6 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
     case LC_HEAD_ROPE_BWD:
     case LC_HEAD_GAIN:
     case LC_COL_SUM: return launch_heads(cls, dtype, t, b, max_blocks, s);
-    case LC_ATTN_RULE_BF16:
-    case LC_ATTN_RULE_BF16 + 1:
-    case LC_ATTN_RULE_BF16 + 2:
-    case LC_ATTN_RULE_BF16_LAST: return launch_attn_rule(cls, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE: return launch_attn_f32(true, true, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_RULE_F32: return launch_attn_f32(false, true, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BWD: return launch_attn_f32(true, false, dtype, head_dim, t, b, max_blocks, s);

@@ -38,11 +38,6 @@ __device__ __forceinline__ int swizzle(int row) {
   return HD == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 2) << 1) | ((row >> 2) & 3);
 }
 
-// tanh where an absolute error of 2^-23 is small beside the rounding of the weights: 1 - 2 / (exp(2 x) + 1)
-__device__ __forceinline__ float tanh_of_scaled(float two_log2e_x) {
-  return __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(two_log2e_x) + 1.f), 1.f);
-}
-
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v = min(v, __shfl_xor(v, off, 64));
@@ -162,72 +157,88 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
     if (kv0 + kRuleKeys < end) issue(kv0 + kRuleKeys, stg ^ 1);
     const char* kb = lds + stg * STAGE;
     const char* vb = kb + KBYTES;
+    if (kv0 + kRuleKeys <= w_begin || kv0 >= w_end) continue;
+    // 64 keys at once: two chains of products, and a weight's way through the vector units in the shadow of the other wavefront's
+    f32x16 s[2];
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      const int kvs = kv0 + sub * 32;
-      if (kvs + 32 <= w_begin || kvs >= w_end) continue;
-      f32x16 s;
+    for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+      for (int r = 0; r < 16; ++r) s[sub][r] = 0.f;
 #pragma unroll
-      for (int j = 0; j < HD / 16; ++j)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kb + sub * 32 * (HD * 2) + k_at + ((2 * j + g) ^ k_sw) * 16), qf[j], s, 0, 0, 0);
-      // register r of this lane: key kvs + 16 (r >> 3) + 8 g + (r & 7)
-      const float base = from_me - (float)(kvs + 8 * g);
+    for (int j = 0; j < HD / 16; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (CAP) s[r] = cap2 * tanh_of_scaled(s[r] * into_tanh);
-        else s[r] *= scale2;
-        if (SLOPES) s[r] = __builtin_fmaf(-slope2, fabsf(base - (float)(16 * (r >> 3) + (r & 7))), s[r]);
-      }
-      float mx = -INFINITY;
-      if (kvs < all_lo || kvs + 32 > all_hi) {
-        const int first = lo - kvs - 8 * g;
-        const uint32_t len = hi - lo;
+      for (int sub = 0; sub < 2; ++sub)
+        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kb + sub * 32 * (HD * 2) + k_at + ((2 * j + g) ^ k_sw) * 16), qf[j], s[sub], 0, 0, 0);
+    // register r of s[sub]: key kv0 + 32 sub + 16 (r >> 3) + 8 g + (r & 7).  A capped score is kept as y = 1 / (1 + exp(2 z / cap)), of which it is
+    // cap (1 - 2 y); one with neither cap nor slope as the product.
+    const float base = from_me - (float)(kv0 + 8 * g);
+    if (CAP || SLOPES) {
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = (uint32_t)(16 * (r >> 3) + (r & 7) - first) < len ? s[r] : -INFINITY;
-          mx = fmaxf(mx, s[r]);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
-      }
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mn = fmaxf(m, mx);
-      // What is summed so far is rescaled only when the maximum of some query of the wavefront has grown by more than kLazyMax (in
-      // units of log2): until then weights are relative to the older maximum and stay below 2^kLazyMax.
-      if (__any(mn > m + kLazyMax)) {
-        const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-        l *= alpha;
-#pragma unroll
-        for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) ot[i][r] *= alpha;
-        m = mn;
-      }
-      const float msub = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight is exp2(-inf) = 0
-      union { uint32_t u[4]; bf16x8 v; } p[2];
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const float pa = __builtin_amdgcn_exp2f(s[r] - msub), pb = __builtin_amdgcn_exp2f(s[r + 1] - msub);
-        l += pa + pb;
-        p[r >> 3].u[(r & 7) >> 1] = f2bf2(pa, pb);
-      }
-      // O^T[d, q] += sum over 16 keys of V^T[d, key] P^T[key, q]
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int i = 0; i < HD / 32; ++i) {
-          union { s16x4 h[2]; bf16x8 v; } a;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = sub * 32 + ks * 16 + 4 * e + v_row;
-            a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + r * (HD * 2) + ((i * 4 + v_piece) ^ swizzle<HD>(r)) * 16 + v_in));
+          float x = s[sub][r];
+          if (CAP) x = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * into_tanh) + 1.f);
+          if (SLOPES) {
+            x = CAP ? __builtin_fmaf(-2.f * cap2, x, cap2) : x * scale2;
+            x = __builtin_fmaf(-slope2, fabsf(base - (float)(32 * sub + 16 * (r >> 3) + (r & 7))), x);
           }
-          ot[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[ks].v, ot[i], 0, 0, 0);
+          s[sub][r] = x;
         }
     }
+    constexpr bool LOW = CAP && !SLOPES;  // the largest score is the smallest y
+    if (kv0 < all_lo || kv0 + kRuleKeys > all_hi) {
+      const int first = lo - kv0 - 8 * g;
+      const uint32_t len = hi - lo;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[sub][r] = (uint32_t)(32 * sub + 16 * (r >> 3) + (r & 7) - first) < len ? s[sub][r] : LOW ? INFINITY : -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int r = 1; r < 32; ++r) mx = LOW ? fminf(mx, s[r >> 4][r & 15]) : fmaxf(mx, s[r >> 4][r & 15]);
+    {
+      const float other = __shfl_xor(mx, 32, 64);
+      mx = LOW ? fminf(mx, other) : fmaxf(mx, other);
+    }
+    const float factor = SLOPES ? 1.f : CAP ? -2.f * cap2 : scale2, offset = LOW ? cap2 : 0.f;  // a score in units of log2: factor * s + offset
+    const float mn = fmaxf(m, SLOPES ? mx : __builtin_fmaf(mx, factor, offset));
+    // What is summed so far is rescaled only when the maximum of some query of the wavefront has grown by more than kLazyMax (in
+    // units of log2): until then weights are relative to the older maximum and stay below 2^kLazyMax.
+    if (__any(mn > m + kLazyMax)) {
+      const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ot[i][r] *= alpha;
+      m = mn;
+    }
+    const float msub = offset - (m == -INFINITY ? 0.f : m);  // nothing seen yet: every weight is exp2(-inf) = 0
+    union { uint32_t u[4]; bf16x8 v; } p[4];
+#pragma unroll
+    for (int r = 0; r < 32; r += 2) {
+      const float sa = s[r >> 4][r & 15], sb = s[r >> 4][(r & 15) + 1];
+      const float pa = __builtin_amdgcn_exp2f(SLOPES ? sa + msub : __builtin_fmaf(sa, factor, msub));
+      const float pb = __builtin_amdgcn_exp2f(SLOPES ? sb + msub : __builtin_fmaf(sb, factor, msub));
+      l += pa + pb;
+      p[r >> 3].u[(r & 7) >> 1] = f2bf2(pa, pb);
+    }
+    // O^T[d, q] += sum over 16 keys of V^T[d, key] P^T[key, q]
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) {
+        union { s16x4 h[2]; bf16x8 v; } a;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int r = ks * 16 + 4 * e + v_row;
+          a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + r * (HD * 2) + ((i * 4 + v_piece) ^ swizzle<HD>(r)) * 16 + v_in));
+        }
+        ot[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[ks].v, ot[i], 0, 0, 0);
+      }
   }
   // a weight of zero times an infinity or NaN of a key the row does not see: such rows are formed again
   float z = 0.f;

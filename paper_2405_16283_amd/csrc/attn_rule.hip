@@ -21,6 +21,7 @@
 #include "attn_rows.h"
 
 #include <climits>
+#include <type_traits>
 
 namespace tn {
 namespace {
@@ -30,6 +31,7 @@ constexpr int kRuleKeys = 64;   // keys per stage
 constexpr float kLazyMax = 8.f; // see the rescaling step
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+typedef __attribute__((address_space(3))) const bf16x8* lds_bf16x8;
 
 // Where piece `piece` (16 bytes) of a row of 2 HD bytes is stored: reads of one piece of 16 rows, and of 4 pieces of 4 rows, fall on
 // different banks.
@@ -144,20 +146,25 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
   const float from_me = (float)(rule.q_pos0 + row - rule.k_pos0);  // distance of the block's first key
   const int a_ = l32 >> 3, b_ = l32 & 3, g_ = (l32 >> 2) & 1;
   const int kperm = 16 * (a_ >> 1) + 8 * g_ + 4 * (a_ & 1) + b_;
-  // fragment addresses inside a stage.  K: row sub * 32 + kperm (whose swizzle sub leaves alone), piece 2 s + g.  V: rows 8 g + 4 i +
-  // (lane & 15) / 4 of a slab of 16 keys, 16 columns from 16 * (lane >> 4 & 1), 4 of them from 4 * (lane & 3).
-  const int k_at = kperm * (HD * 2), k_sw = swizzle<HD>(kperm);
-  const int v_row = 8 * g + ((lane & 15) >> 2), v_piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), v_in = (lane & 1) * 8;
-
-  if (begin < end) issue(begin, 0);
-  int stg = 0;
-  for (int kv0 = begin; kv0 < end; kv0 += kRuleKeys, stg ^= 1) {
+  // Fragment addresses in the first stage, formed once: what a chunk adds to them is constant.  K: row 32 sub + kperm (whose swizzle sub
+  // leaves alone), piece 2 j + g.  V: rows 16 ks + 8 g + 4 e + (lane & 15) / 4, 16 columns from 16 * (lane >> 4 & 1) of 32 i, 4 of
+  // them from 4 * (lane & 3); the swizzle of those rows depends on e only.
+  uint32_t k_at[HD / 16], v_at[2][HD / 32];
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) k_at[j] = lds0 + kperm * (HD * 2) + ((2 * j + g) ^ swizzle<HD>(kperm)) * 16;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) {
+      const int r = 8 * g + 4 * e + ((lane & 15) >> 2), piece = 4 * i + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      v_at[e][i] = lds0 + KBYTES + r * (HD * 2) + (piece ^ swizzle<HD>(r)) * 16 + (lane & 1) * 8;
+    }
+  auto chunk = [&](int kv0, auto stage) {
+    constexpr int at = decltype(stage)::value * STAGE;
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this chunk has arrived
     __syncthreads();                     // ... for everybody, and everybody is done with the other stage
-    if (kv0 + kRuleKeys < end) issue(kv0 + kRuleKeys, stg ^ 1);
-    const char* kb = lds + stg * STAGE;
-    const char* vb = kb + KBYTES;
-    if (kv0 + kRuleKeys <= w_begin || kv0 >= w_end) continue;
+    if (kv0 + kRuleKeys < end) issue(kv0 + kRuleKeys, 1 - decltype(stage)::value);
+    if (kv0 + kRuleKeys <= w_begin || kv0 >= w_end) return;
     // 64 keys at once: two chains of products, and a weight's way through the vector units in the shadow of the other wavefront's
     f32x16 s[2];
 #pragma unroll
@@ -168,7 +175,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
     for (int j = 0; j < HD / 16; ++j)
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
-        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kb + sub * 32 * (HD * 2) + k_at + ((2 * j + g) ^ k_sw) * 16), qf[j], s[sub], 0, 0, 0);
+        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8)(size_t)(k_at[j] + (at + sub * 32 * (HD * 2))), qf[j], s[sub], 0, 0, 0);
     // register r of s[sub]: key kv0 + 32 sub + 16 (r >> 3) + 8 g + (r & 7).  A capped score is kept as y = 1 / (1 + exp(2 z / cap)), of which it is
     // cap (1 - 2 y); one with neither cap nor slope as the product.
     const float base = from_me - (float)(kv0 + 8 * g);
@@ -188,7 +195,8 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
     }
     constexpr bool LOW = CAP && !SLOPES;  // the largest score is the smallest y
     if (kv0 < all_lo || kv0 + kRuleKeys > all_hi) {
-      const int first = lo - kv0 - 8 * g;
+      int first = lo - kv0 - 8 * g;
+      asm volatile("" : "+v"(first));  // a branch, not 64 selects on every chunk
       const uint32_t len = hi - lo;
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
@@ -233,12 +241,14 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
       for (int i = 0; i < HD / 32; ++i) {
         union { s16x4 h[2]; bf16x8 v; } a;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int r = ks * 16 + 4 * e + v_row;
-          a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + r * (HD * 2) + ((i * 4 + v_piece) ^ swizzle<HD>(r)) * 16 + v_in));
-        }
+        for (int e = 0; e < 2; ++e) a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(size_t)(v_at[e][i] + (at + ks * 16 * (HD * 2))));
         ot[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[ks].v, ot[i], 0, 0, 0);
       }
+  };
+  if (begin < end) issue(begin, 0);
+  for (int kv0 = begin; kv0 < end; kv0 += 2 * kRuleKeys) {
+    chunk(kv0, std::integral_constant<int, 0>{});
+    if (kv0 + kRuleKeys < end) chunk(kv0 + kRuleKeys, std::integral_constant<int, 1>{});
   }
   // a weight of zero times an infinity or NaN of a key the row does not see: such rows are formed again
   float z = 0.f;
@@ -433,19 +443,23 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
 
   const int a_ = l32 >> 3, b_ = l32 & 3, g_ = (l32 >> 2) & 1;
   const int perm = 16 * (a_ >> 1) + 8 * g_ + 4 * (a_ & 1) + b_;
-  const int k_at = perm * (HD * 2), k_sw = swizzle<HD>(perm);
-  const int v_row = 8 * g + ((lane & 15) >> 2), v_piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), v_in = (lane & 1) * 8;
+  // fragment addresses in the first stage, as in the forward kernel; V^T's place is taken by the chunk that the gradient is summed from
+  uint32_t k_at[HD / 16], v_at[2][HD / 32];
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) k_at[j] = lds0 + perm * (HD * 2) + ((2 * j + g) ^ swizzle<HD>(perm)) * 16;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) {
+      const int r = 8 * g + 4 * e + ((lane & 15) >> 2), piece = 4 * i + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      v_at[e][i] = lds0 + (MODE == 3 ? ABYTES : 0) + r * (HD * 2) + (piece ^ swizzle<HD>(r)) * 16 + (lane & 1) * 8;
+    }
   const float from_me = (float)(rule.q_pos0 - rule.k_pos0 + (OWN_Q ? row : -row));  // query position - key position, less the other side's index
 
-  if (begin < end) {
-    issue(begin, 0);
-    load_stats(begin);
-  }
-  int stg = 0;
-  for (int o0 = begin; o0 < end; o0 += CH, stg ^= 1) {
+  auto chunk = [&](int o0, auto which) {
+    constexpr int stg = decltype(which)::value, at0 = stg * STAGE;
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this chunk and its statistics have arrived
-    char* const stage = lds + stg * STAGE;
-    float* const st = (float*)(stage + 2 * ABYTES);
+    float* const st = (float*)(lds + at0 + 2 * ABYTES);
     if (!OWN_Q && threadIdx.x < CH) {
       st[threadIdx.x] = s_start;
       st[CH + threadIdx.x] = s_D;
@@ -454,10 +468,10 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
     }
     __syncthreads();  // ... for everybody, and everybody is done with the other stage
     if (o0 + CH < end) {
-      issue(o0 + CH, stg ^ 1);
+      issue(o0 + CH, 1 - stg);
       load_stats(o0 + CH);
     }
-#pragma unroll 1
+#pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
       const int os = o0 + sub * 32;
       bool all_see;
@@ -469,7 +483,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
         if (!__any(ql < key1 && qh > key0)) continue;
         all_see = __all(ql <= key0 && qh >= row0 + 32);
       }
-      const char* ra = stage + sub * 32 * (HD * 2) + k_at;
+      constexpr int slab = 32 * (HD * 2);
       f32x16 s, dp;
       // register r: row os + 16 (r >> 3) + 8 g + (r & 7) of the other side
       float starts[16];
@@ -490,9 +504,8 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
       }
 #pragma unroll
       for (int j = 0; j < HD / 16; ++j) {
-        const int at = ((2 * j + g) ^ k_sw) * 16;
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(ra + at), mine[j], s, 0, 0, 0);
-        if (MODE != 3) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(ra + ABYTES + at), mine2[j], dp, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8)(size_t)(k_at[j] + (at0 + sub * slab)), mine[j], s, 0, 0, 0);
+        if (MODE != 3) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8)(size_t)(k_at[j] + (at0 + ABYTES + sub * slab)), mine2[j], dp, 0, 0, 0);
       }
       const float base = from_me + (OWN_Q ? -(float)(os + 8 * g) : (float)(os + 8 * g));
       float pr[16];
@@ -514,7 +527,8 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
       }
       if (!all_see) {
         if (OWN_Q) {
-          const int first = lo - os - 8 * g;
+          int first = lo - os - 8 * g;
+          asm volatile("" : "+v"(first));  // a branch, not selects on every slab
           const uint32_t len = hi - lo;
 #pragma unroll
           for (int r = 0; r < 16; ++r) pr[r] = (uint32_t)(16 * (r >> 3) + (r & 7) - first) < len ? pr[r] : 0.f;
@@ -529,20 +543,24 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
       union { uint32_t u[4]; bf16x8 v; } p[2];
 #pragma unroll
       for (int r = 0; r < 16; r += 2) p[r >> 3].u[(r & 7) >> 1] = f2bf2(pr[r], pr[r + 1]);
-      const char* const tb = stage + (MODE == 3 ? ABYTES : 0);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int i = 0; i < HD / 32; ++i) {
           union { s16x4 h[2]; bf16x8 v; } a;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = ks * 16 + 4 * e + v_row;  // (sub * 32 leaves the swizzle alone)
-            a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(tb + sub * 32 * (HD * 2) + r * (HD * 2) + ((i * 4 + v_piece) ^ swizzle<HD>(r)) * 16 + v_in));
-          }
+          for (int e = 0; e < 2; ++e) a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(size_t)(v_at[e][i] + (at0 + sub * slab + ks * 16 * (HD * 2))));
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[ks].v, acc[i], 0, 0, 0);
         }
     }
+  };
+  if (begin < end) {
+    issue(begin, 0);
+    load_stats(begin);
+  }
+  for (int o0 = begin; o0 < end; o0 += 2 * CH) {
+    chunk(o0, std::integral_constant<int, 0>{});
+    if (o0 + CH < end) chunk(o0 + CH, std::integral_constant<int, 1>{});
   }
   // a weight of zero times an infinity or NaN of a row that does not matter to this one: such rows are formed again
   float z = 0.f;

@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   int lo = 0, hi = 0;  // RULE: what this lane's query sees
   Seen seen{};
   float slope = 0.f;
+  const Rule rule = RULE ? Rule(t, d) : Rule();
   if constexpr (RULE) {
-    const Rule rule(t, d);
     if (row < q_rows) rule.visible(row, lo, hi);
     seen = seen_by_all(lo, hi, row < q_rows, (int*)lds);
     begin = seen.begin < seen.end ? seen.begin & ~(kRows - 1) : 0;
@@ -235,14 +235,27 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
     // element i of s[k]: key kv0 + 16 k + 4 g + i
     float mx = -INFINITY;
     const bool mask = kv0 + kRows > kv_rows || (causal && k_pos0 + kv0 + kRows - 1 > wpos0);
+    if constexpr (RULE) {
+      if (rule.cap > 0.f) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[k][i] = rule.cap * tanh_f32(s[k][i] * rule.inv_cap);
+      }
+      if (rule.slopes) {
+        const float base = (float)(qpos - k_pos0 - kv0 - 4 * g);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[k][i] = fmaf(-slope, fabsf(base - (float)(16 * k + i)), s[k][i]);
+      }
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int kv = kv0 + 16 * k + 4 * g + i;
         if constexpr (RULE) {
-          float th;
-          s[k][i] = Rule(t, d).score(s[k][i], slope, qpos - k_pos0 - kv, th);
           if (kv < lo || kv >= hi) s[k][i] = -INFINITY;
         } else {
           if (mask && (kv >= kv_rows || (causal && k_pos0 + kv > qpos))) s[k][i] = -INFINITY;
@@ -355,8 +368,8 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
   int lo = 0, hi = 0;  // RULE, mode 1: what this lane's query sees
   Seen seen{};
   float slope = 0.f;
+  const Rule rule = RULE ? Rule(t, d) : Rule();
   if constexpr (RULE) {
-    const Rule rule(t, d);
     slope = rule.slope(h);
     if (MODE == 1) {
       if (row < my_rows) rule.visible(row, lo, hi);
@@ -370,7 +383,7 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
     bool all_see = true;  // RULE, modes 2 and 3: every query of the chunk sees every key of the workgroup
     if constexpr (RULE && MODE >= 2) {
       int ql = 0, qh = 0;  // lane by lane the chunk's queries; every wavefront finds the same
-      if (r0 + lane < q_rows) Rule(t, d).visible(r0 + lane, ql, qh);
+      if (r0 + lane < q_rows) rule.visible(r0 + lane, ql, qh);
       const int k0 = rb * kRows, k1 = min(k0 + kRows, kv_rows);
       if (!__any(max(ql, k0) < min(qh, k1))) continue;
       all_see = __all(ql <= k0 && qh >= k1);
@@ -431,7 +444,7 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
           float z = s[e][i] * scale, th = 0.f;
           if constexpr (RULE) {
             ok = MODE == 1 ? o >= lo && o < hi : row >= sees[lr][0] && row < sees[lr][1];
-            z = Rule(t, d).score(z, slope, MODE == 1 ? pos - d.p.k_pos0 - o : d.p.q_pos0 + o - pos, th);
+            z = rule.score(z, slope, MODE == 1 ? pos - d.p.k_pos0 - o : d.p.q_pos0 + o - pos, th);
           } else {
             if (causal) ok = ok && (MODE <= 1 ? d.p.k_pos0 + o <= pos : pos <= d.p.q_pos0 + o);
           }

@@ -73,8 +73,8 @@ __device__ __forceinline__ void attn_by_rows(DeviceTables t, const OpDesc& d, in
     float m = -INFINITY, l = 0.f;
     int from = 0, seen = min(K.rows, d.p.q_pos0 + row - d.p.k_pos0 + 1);
     float slope = 0.f;
+    const Rule rule = RULE ? Rule(t, d) : Rule();
     if constexpr (RULE) {
-      const Rule rule(t, d);
       rule.visible(row, from, seen);
       slope = rule.slope(h);
     }
@@ -86,7 +86,7 @@ __device__ __forceinline__ void attn_by_rows(DeviceTables t, const OpDesc& d, in
       s = row_sum(s);
       if constexpr (RULE) {
         float th;
-        s = Rule(t, d).score(s, slope, d.p.q_pos0 + row - d.p.k_pos0 - k, th);
+        s = rule.score(s, slope, d.p.q_pos0 + row - d.p.k_pos0 - k, th);
       }
       const float mn = fmaxf(m, s), ms = mn == -INFINITY ? 0.f : mn;
       const float alpha = __expf(m - ms), p = __expf(s - ms);
@@ -133,8 +133,8 @@ __device__ __forceinline__ void attn_bwd_by_rows(const DeviceTables& t, const Op
     int begin = MODE == 1 ? 0 : max(0, d.p.k_pos0 + row - d.p.q_pos0);
     int end = MODE == 1 ? min(K.rows, d.p.q_pos0 + row - d.p.k_pos0 + 1) : Q.rows;
     float slope = 0.f;
+    const Rule rule = RULE ? Rule(t, d) : Rule();
     if constexpr (RULE) {
-      const Rule rule(t, d);
       if (MODE == 1) rule.visible(row, begin, end);
       else begin = 0;
       slope = rule.slope(h);
@@ -143,7 +143,7 @@ __device__ __forceinline__ void attn_bwd_by_rows(const DeviceTables& t, const Op
     for (int o = begin; o < end; ++o) {
       if constexpr (RULE && MODE >= 2) {
         int lo, hi;
-        Rule(t, d).visible(o, lo, hi);
+        rule.visible(o, lo, hi);
         if (row < lo || row >= hi) continue;
       }
       float s = 0.f, dp = 0.f;
@@ -154,7 +154,7 @@ __device__ __forceinline__ void attn_bwd_by_rows(const DeviceTables& t, const Op
       }
       const int q = MODE == 1 ? row : o;
       float z = row_sum(s) * d.p.scale, th = 0.f;
-      if constexpr (RULE) z = Rule(t, d).score(z, slope, d.p.q_pos0 + q - d.p.k_pos0 - (MODE == 1 ? o : row), th);
+      if constexpr (RULE) z = rule.score(z, slope, d.p.q_pos0 + q - d.p.k_pos0 - (MODE == 1 ? o : row), th);
       float p = __expf(z - stat(q, 0));
       if (MODE != 3) p *= (row_sum(dp) - stat(q, 1)) * d.p.scale;
       if (RULE && MODE != 3) p *= 1.f - th * th;

@@ -27,6 +27,7 @@ struct Rule {
   const float* slopes;    // of the heads of the column group, or null
   void* const* spans;     // one tensor per Q row tile, or null
   int tq, q_pos0, k_pos0, kv_rows, causal;
+  __device__ Rule() : cap(0.f), inv_cap(0.f), slopes(nullptr), spans(nullptr), tq(1), q_pos0(0), k_pos0(0), kv_rows(0), causal(0) {}
   __device__ Rule(const DeviceTables& t, const OpDesc& d) {
     const int* ax = t.aux + d.aux0;
     cap = __int_as_float(ax[kRuleCap]);

@@ -215,6 +215,290 @@ __global__ void __launch_bounds__(256) head_gain_kernel(DeviceTables t, Batch b)
   for (int c = threadIdx.x; c < s.head_dim; c += 256) o[c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
 }
 
+// ---- heads of a multiple of 16 elements, pairs that come in eights ---------------------------------
+// Eight pairs to a lane -- two runs of eight elements, 16-byte accesses -- and a head to 4, 8, 16 .. lanes, of which those past its end
+// are idle.  What bounds these is memory; a lane's angles, 8 of them with 64-bit products, are formed once for the heads it walks
+// over, as many as leave enough wavefronts to fill the chip (kHeadWalk).
+
+// eight elements as loaded, which may be on their way while the head before them is worked on
+template <typename T>
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> fetch8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.w[k] = ((const uint4*)p)[k];
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&v)[8]) {
+  const uint32_t* w = (const uint32_t*)r.w;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = sizeof(T) == 4 ? __uint_as_float(w[k]) : __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) { unpack8(fetch8(p), v); }
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *(f32x4*)p = (f32x4){v[0], v[1], v[2], v[3]};
+  *(f32x4*)(p + 4) = (f32x4){v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+  *(uint4*)p = make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float exchanged(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+
+// A lane's place in its head: where its two runs begin, and whether its pairs are (run 0, run 1) or neighbours.
+struct Eights {
+  int lanes, j;
+  bool there, apart;  // the lane has pairs; they lie half a rotation apart
+  int first, second;  // elements
+  bool turns;
+  __device__ Eights(const Head& s) {
+    lanes = head_lanes(s.head_dim);
+    j = threadIdx.x & (lanes - 1);
+    there = 16 * j < s.head_dim;
+    turns = 8 * j < s.pairs.half_rotary;
+    apart = s.pairs.half && turns;
+    first = apart ? 8 * j : 16 * j;
+    second = apart ? s.pairs.half_rotary + 8 * j : 16 * j + 8;
+  }
+  __device__ void angles(const Head& s, int row, float (&sn)[8], float (&cs)[8]) const {
+    const double pos = s.position(row);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      sn[k] = 0.f;
+      cs[k] = 1.f;
+      if (there && 8 * j + k < s.pairs.half_rotary) turn(pos, s.turns[8 * j + k], sn[k], cs[k]);
+    }
+  }
+  // over the lanes of a head.  Within 16 lanes by exchanges inside the vector unit: neighbours, pairs, then the mirrored half
+  __device__ float sum(float v) const {
+    if (lanes > 1) v += exchanged<0xB1>(v);
+    if (lanes > 2) v += exchanged<0x4E>(v);
+    if (lanes > 4) v += exchanged<0x141>(v);
+    if (lanes > 8) v += exchanged<0x140>(v);
+    for (int off = 16; off < lanes; off <<= 1) v += __shfl_xor(v, off, 64);
+    return v;
+  }
+};
+
+// (u, v) turned in place
+template <bool APART>
+__device__ __forceinline__ void rotate8(float (&u)[8], float (&v)[8], const float (&sn)[8], const float (&cs)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float& a = APART ? u[k] : k < 4 ? u[2 * k] : v[2 * k - 8];
+    float& b = APART ? v[k] : k < 4 ? u[2 * k + 1] : v[2 * k - 7];
+    const float x = a, y = b;
+    a = x * cs[k] - y * sn[k];
+    b = x * sn[k] + y * cs[k];
+  }
+}
+
+// Where a lane of the grid starts: its row, and the first of the kHeadWalk heads that it walks over.
+struct Walk {
+  int row, h0, h1;
+  bool any;
+  __device__ Walk(const Head& s, int lanes) {
+    const int walk = s.ax[kHeadWalk], runs = (s.heads + walk - 1) / walk;
+    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+    any = id < (int64_t)s.rows * runs;
+    row = any ? (int)(id % s.rows) : 0;
+    h0 = any ? (int)(id / s.rows) * walk : 0;
+    h1 = any ? min(s.heads, h0 + walk) : 0;
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) head_rope_eights_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  const Head s(t, d);
+  const Eights e(s);
+  const Walk at(s, e.lanes);
+  const bool on = e.there && at.any;
+  const T* x = (const T*)t.ptrs[d.ptr0] + (size_t)at.row * s.cols;
+  T* o = (T*)d.out + (size_t)at.row * s.cols;
+  float ga[8], gb[8], sn[8], cs[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) ga[k] = gb[k] = 1.f;
+  if (s.norm && on) {
+    load8((const T*)t.ptrs[d.ptr0 + 1] + e.first, ga);
+    load8((const T*)t.ptrs[d.ptr0 + 1] + e.second, gb);
+  }
+  e.angles(s, at.row, sn, cs);
+  if (d.p.mode) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sn[k] = -sn[k];
+  }
+  Raw8<T> nu{}, nv{};
+  auto fetch = [&](int h) {
+    if (!on) return;
+    nu = fetch8(x + (size_t)h * s.head_dim + e.first);
+    nv = fetch8(x + (size_t)h * s.head_dim + e.second);
+  };
+  if (at.h0 < at.h1) fetch(at.h0);
+  for (int h = at.h0; h < at.h1; ++h) {
+    const Raw8<T> ru = nu, rv = nv;
+    if (h + 1 < at.h1) fetch(h + 1);
+    float u[8], v[8];
+    unpack8(ru, u);
+    unpack8(rv, v);
+    if (s.norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ss += u[k] * u[k] + v[k] * v[k];
+      const float r = s.rstd(e.sum(ss));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        u[k] *= r * ga[k];
+        v[k] *= r * gb[k];
+      }
+    }
+    if (e.apart) rotate8<true>(u, v, sn, cs);
+    else rotate8<false>(u, v, sn, cs);
+    if (on) {
+      store8(o + (size_t)h * s.head_dim + e.first, u);
+      store8(o + (size_t)h * s.head_dim + e.second, v);
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) head_rope_bwd_eights_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  const Head s(t, d);
+  const Eights e(s);
+  const Walk at(s, e.lanes);
+  const bool on = e.there && at.any;
+  const T* dy = (const T*)t.ptrs[d.ptr0] + (size_t)at.row * s.cols;
+  const T* x = (const T*)t.ptrs[d.ptr0 + 1] + (size_t)at.row * s.cols;
+  T* o = (T*)d.out + (size_t)at.row * s.cols;
+  float ga[8] = {}, gb[8] = {}, sn[8], cs[8];
+  if (on) {
+    load8((const T*)t.ptrs[d.ptr0 + 2] + e.first, ga);
+    load8((const T*)t.ptrs[d.ptr0 + 2] + e.second, gb);
+  }
+  e.angles(s, at.row, sn, cs);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sn[k] = -sn[k];
+  Raw8<T> nu{}, nv{}, np{}, nq{};
+  auto fetch = [&](int h) {
+    if (!on) return;
+    const size_t c = (size_t)h * s.head_dim;
+    nu = fetch8(dy + c + e.first);
+    nv = fetch8(dy + c + e.second);
+    np = fetch8(x + c + e.first);
+    nq = fetch8(x + c + e.second);
+  };
+  if (at.h0 < at.h1) fetch(at.h0);
+  for (int h = at.h0; h < at.h1; ++h) {
+    const Raw8<T> ru = nu, rv = nv, rp = np, rq = nq;
+    if (h + 1 < at.h1) fetch(h + 1);
+    float u[8], v[8], p[8], q[8];
+    unpack8(ru, u);
+    unpack8(rv, v);
+    unpack8(rp, p);
+    unpack8(rq, q);
+    if (e.apart) rotate8<true>(u, v, sn, cs);
+    else rotate8<false>(u, v, sn, cs);
+    float ss = 0.f, dot = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      u[k] *= ga[k];
+      v[k] *= gb[k];
+      ss += p[k] * p[k] + q[k] * q[k];
+      dot += u[k] * p[k] + v[k] * q[k];
+    }
+    const float r = s.rstd(e.sum(ss)), m = e.sum(dot) * r * r / (float)s.head_dim;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      u[k] = r * (u[k] - p[k] * m);
+      v[k] = r * (v[k] - q[k] * m);
+    }
+    if (on) {
+      store8(o + (size_t)h * s.head_dim + e.first, u);
+      store8(o + (size_t)h * s.head_dim + e.second, v);
+    }
+  }
+}
+
+// Sums of the gain's gradient: the lanes of a head keep to one row at a time and walk over its heads; what the groups of a wavefront
+// and the wavefronts of the workgroup have summed is added in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(256) head_gain_eights_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  const Head s(t, d);
+  const Eights e(s);
+  __shared__ float part[4][1024];
+  const int row0 = blockIdx.x * kGainRows, n = min(kGainRows, s.rows - row0);
+  const int groups = 256 / e.lanes, group = threadIdx.x / e.lanes;
+  const int per_row = max(1, groups / kGainRows);  // groups that share a row
+  float ga[8] = {}, gb[8] = {};
+  for (int r = group / per_row; r < n; r += groups / per_row) {
+    const T* dy = (const T*)t.ptrs[d.ptr0] + (size_t)(row0 + r) * s.cols;
+    const T* x = (const T*)t.ptrs[d.ptr0 + 1] + (size_t)(row0 + r) * s.cols;
+    float sn[8], cs[8];
+    e.angles(s, row0 + r, sn, cs);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sn[k] = -sn[k];
+    Raw8<T> nu{}, nv{}, np{}, nq{};
+    auto fetch = [&](int h) {
+      if (!e.there) return;
+      const size_t c = (size_t)h * s.head_dim;
+      nu = fetch8(dy + c + e.first);
+      nv = fetch8(dy + c + e.second);
+      np = fetch8(x + c + e.first);
+      nq = fetch8(x + c + e.second);
+    };
+    if (group % per_row < s.heads) fetch(group % per_row);
+    for (int h = group % per_row; h < s.heads; h += per_row) {
+      const Raw8<T> ru = nu, rv = nv, rp = np, rq = nq;
+      if (h + per_row < s.heads) fetch(h + per_row);
+      float u[8], v[8], p[8], q[8];
+      unpack8(ru, u);
+      unpack8(rv, v);
+      unpack8(rp, p);
+      unpack8(rq, q);
+      if (e.apart) rotate8<true>(u, v, sn, cs);
+      else rotate8<false>(u, v, sn, cs);
+      float ss = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ss += p[k] * p[k] + q[k] * q[k];
+      const float rstd = s.rstd(e.sum(ss));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        ga[k] = fmaf(u[k], p[k] * rstd, ga[k]);
+        gb[k] = fmaf(v[k], q[k] * rstd, gb[k]);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    for (int off = e.lanes; off < 64; off <<= 1) {
+      ga[k] += __shfl_xor(ga[k], off, 64);
+      gb[k] += __shfl_xor(gb[k], off, 64);
+    }
+  if ((int)(threadIdx.x & 63) < e.lanes && e.there) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      part[threadIdx.x >> 6][e.first + k] = ga[k];
+      part[threadIdx.x >> 6][e.second + k] = gb[k];
+    }
+  }
+  __syncthreads();
+  float* o = (float*)d.out + (size_t)blockIdx.x * s.head_dim;
+  for (int c = threadIdx.x; c < s.head_dim; c += 256) o[c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+}
+
 // Sum of all rows of the operands: a workgroup per 32 columns, eight threads to a column, each every eighth row; their sums are
 // added in order.
 __global__ void __launch_bounds__(256) col_sum_kernel(DeviceTables t, Batch b) {
@@ -244,10 +528,15 @@ __global__ void __launch_bounds__(256) col_sum_kernel(DeviceTables t, Batch b) {
 
 int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   const int32_t* ax = aux + d.aux0;
+  const int64_t heads = cls == LC_COL_SUM ? 0 : ax[kHeadCols] / d.p.head_dim;
   switch (cls) {
     case LC_HEAD_ROPE:
-    case LC_HEAD_ROPE_BWD: return (int32_t)(((int64_t)ax[kHeadRows] * (ax[kHeadCols] / d.p.head_dim) + 3) / 4);
-    case LC_HEAD_GAIN: return d.rows;
+    case LC_HEAD_ROPE_BWD: return (int32_t)((ax[kHeadRows] * heads + 3) / 4);
+    case LC_HEAD_ROPE_EIGHTS:
+    case LC_HEAD_ROPE_BWD_EIGHTS:
+      return (int32_t)((ax[kHeadRows] * ((heads + ax[kHeadWalk] - 1) / ax[kHeadWalk]) * head_lanes(d.p.head_dim) + 255) / 256);
+    case LC_HEAD_GAIN:
+    case LC_HEAD_GAIN_EIGHTS: return d.rows;
     default: return (d.cols + 31) / 32;
   }
 }
@@ -255,22 +544,22 @@ int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux) {
 hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
   const dim3 grid((unsigned)max_blocks, (unsigned)b.n), wg(256);
   const bool bf = dtype == TN_BF16;
+#define TN_LAUNCH(kernel)                                              \
+  do {                                                                 \
+    if (bf) hipLaunchKernelGGL(kernel<bf16_t>, grid, wg, 0, s, t, b);  \
+    else hipLaunchKernelGGL(kernel<float>, grid, wg, 0, s, t, b);      \
+  } while (0)
   switch (cls) {
-    case LC_HEAD_ROPE:
-      if (bf) hipLaunchKernelGGL(head_rope_kernel<bf16_t>, grid, wg, 0, s, t, b);
-      else hipLaunchKernelGGL(head_rope_kernel<float>, grid, wg, 0, s, t, b);
-      break;
-    case LC_HEAD_ROPE_BWD:
-      if (bf) hipLaunchKernelGGL(head_rope_bwd_kernel<bf16_t>, grid, wg, 0, s, t, b);
-      else hipLaunchKernelGGL(head_rope_bwd_kernel<float>, grid, wg, 0, s, t, b);
-      break;
-    case LC_HEAD_GAIN:
-      if (bf) hipLaunchKernelGGL(head_gain_kernel<bf16_t>, grid, wg, 0, s, t, b);
-      else hipLaunchKernelGGL(head_gain_kernel<float>, grid, wg, 0, s, t, b);
-      break;
+    case LC_HEAD_ROPE: TN_LAUNCH(head_rope_kernel); break;
+    case LC_HEAD_ROPE_BWD: TN_LAUNCH(head_rope_bwd_kernel); break;
+    case LC_HEAD_GAIN: TN_LAUNCH(head_gain_kernel); break;
+    case LC_HEAD_ROPE_EIGHTS: TN_LAUNCH(head_rope_eights_kernel); break;
+    case LC_HEAD_ROPE_BWD_EIGHTS: TN_LAUNCH(head_rope_bwd_eights_kernel); break;
+    case LC_HEAD_GAIN_EIGHTS: TN_LAUNCH(head_gain_eights_kernel); break;
     case LC_COL_SUM: hipLaunchKernelGGL(col_sum_kernel, grid, wg, 0, s, t, b); break;
     default: return hipErrorInvalidValue;
   }
+#undef TN_LAUNCH
   return hipGetLastError();
 }
 

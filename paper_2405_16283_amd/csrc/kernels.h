@@ -84,6 +84,9 @@ enum LaunchClass {
   LC_HEAD_ROPE,      // norm and rotation of heads, any size
   LC_HEAD_ROPE_BWD,  // gradient of their input
   LC_HEAD_GAIN,      // sums of their gain's gradient
+  LC_HEAD_ROPE_EIGHTS, // the three for heads of a multiple of 16 elements
+  LC_HEAD_ROPE_BWD_EIGHTS,
+  LC_HEAD_GAIN_EIGHTS,
   LC_COL_SUM,
   LC_ATTN_RULE_F32,  // attention with a score rule or finished rows, fp32 products
   LC_ATTN_BWD_RULE,  // its gradients, fp32 products
@@ -213,8 +216,23 @@ int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux);
 hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
 // LC_HEAD_ROPE to LC_COL_SUM: heads.hip.  Auxiliary integers of the first three (of LC_COL_SUM: rows per operand):
-enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadAux };
+enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadWalk, kHeadAux };
 constexpr int kGainRows = 32;  // rows to a sum of the gain's gradient
+// Heads of a multiple of 16 elements whose pairs come in eights go to the kernels for those: 16 elements to a lane, a head to a power of
+// two of lanes.  A lane's angles serve all the heads of its row that it walks over; it walks over fewer where there are few
+// rows, down to one, so that the chip has wavefronts enough.
+constexpr int64_t kHeadLanes = 1 << 18;
+inline bool head_by_eights(const int32_t* ax, int32_t head_dim) { return head_dim % 16 == 0 && (!ax[kHeadHalf] || ax[kHeadRotary] % 16 == 0); }
+__host__ __device__ inline int head_lanes(int head_dim) {
+  int n = 1;
+  while (n * 16 < head_dim) n *= 2;
+  return n;
+}
+inline int32_t head_walk(int64_t rows, int32_t heads, int32_t head_dim) {
+  int32_t walk = 8;
+  while (walk > 1 && rows * ((heads + walk - 1) / walk) * head_lanes(head_dim) < kHeadLanes) walk /= 2;
+  return walk;
+}
 int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux);
 hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 

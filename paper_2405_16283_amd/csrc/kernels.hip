@@ -1321,6 +1321,9 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
     case LC_HEAD_ROPE:
     case LC_HEAD_ROPE_BWD:
     case LC_HEAD_GAIN:
+    case LC_HEAD_ROPE_EIGHTS:
+    case LC_HEAD_ROPE_BWD_EIGHTS:
+    case LC_HEAD_GAIN_EIGHTS:
     case LC_COL_SUM: return head_blocks(cls, d, aux);
     case LC_ATTN_STATS: return cdiv((int64_t)d.rows * (d.p.n_col_tiles * aux[d.aux0 + 2] / d.p.head_dim), 16);
     case LC_ATTN_LSE: return cdiv((int64_t)d.rows * d.cols, 256);
@@ -1465,6 +1468,9 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
     case LC_HEAD_ROPE:
     case LC_HEAD_ROPE_BWD:
     case LC_HEAD_GAIN:
+    case LC_HEAD_ROPE_EIGHTS:
+    case LC_HEAD_ROPE_BWD_EIGHTS:
+    case LC_HEAD_GAIN_EIGHTS:
     case LC_COL_SUM: return launch_heads(cls, dtype, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE: return launch_attn_f32(true, true, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_RULE_F32: return launch_attn_f32(false, true, dtype, head_dim, t, b, max_blocks, s);

@@ -18,6 +18,7 @@
 #include "attn_rows.h"
 
 #include <climits>
+#include <type_traits>
 
 namespace tn {
 namespace {
@@ -84,6 +85,18 @@ __device__ __forceinline__ void store_chunk_vt(float (*buf)[kRows + 4], const f3
   for (int i = 0; i < N; ++i) {
     const int p = (I0 + i) * 256 + threadIdx.x;
     *(f32x4*)&buf[p / 16][(p % 16) * 4] = v[i];
+  }
+}
+
+// V by rows as stored (pieces as load_chunk has them), turned round on its way into LDS.  (Fetched by columns, element by element, 1024
+// positions of 16 heads of 64 took 150 us; so 100.)
+template <int HD, int I0 = 0, int N = kPieces(HD)>
+__device__ __forceinline__ void store_chunk_turned(float (*buf)[kRows + 4], const f32x4 (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int p = (I0 + i) * 256 + threadIdx.x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) buf[p % (HD / 4) * 4 + e][p / (HD / 4)] = v[i][e];
   }
 }
 
@@ -190,28 +203,40 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   constexpr bool kAhead = HD == 64;
   constexpr int P = kAhead ? kPieces(HD) : kPieces(HD) / 2;
   f32x4 kn[P], vn[P];
+  auto load_v = [&](int kv0, auto from) {
+    constexpr int I0 = decltype(from)::value;
+    if (v_trans) load_chunk_vt<T, HD, I0, P>(V, true, kv0, vn);
+    else load_chunk<T, HD, I0, P>(V, false, kv0, vn);
+  };
+  auto store_v = [&](auto from) {
+    constexpr int I0 = decltype(from)::value;
+    if (v_trans) store_chunk_vt<HD, I0, P>(vs, vn);
+    else store_chunk_turned<HD, I0, P>(vs, vn);
+  };
+  constexpr std::integral_constant<int, 0> kFirst{};
+  constexpr std::integral_constant<int, P> kRest{};
   if (kAhead && end > begin) {
     load_chunk<T, HD, 0, P>(K, false, begin, kn);
-    load_chunk_vt<T, HD, 0, P>(V, v_trans, begin, vn);
+    load_v(begin, kFirst);
   }
   for (int kv0 = begin; kv0 < end; kv0 += kRows) {
     __syncthreads();  // everybody is done with the chunk before
     if constexpr (!kAhead) {
       load_chunk<T, HD, 0, P>(K, false, kv0, kn);
-      load_chunk_vt<T, HD, 0, P>(V, v_trans, kv0, vn);
+      load_v(kv0, kFirst);
     }
     store_chunk<HD, 0, P>(ks, kn);
-    store_chunk_vt<HD, 0, P>(vs, vn);
+    store_v(kFirst);
     if constexpr (!kAhead) {
       load_chunk<T, HD, P, P>(K, false, kv0, kn);
-      load_chunk_vt<T, HD, P, P>(V, v_trans, kv0, vn);
+      load_v(kv0, kRest);
       store_chunk<HD, P, P>(ks, kn);
-      store_chunk_vt<HD, P, P>(vs, vn);
+      store_v(kRest);
     }
     __syncthreads();
     if (kAhead && kv0 + kRows < end) {
       load_chunk<T, HD, 0, P>(K, false, kv0 + kRows, kn);
-      load_chunk_vt<T, HD, 0, P>(V, v_trans, kv0 + kRows, vn);
+      load_v(kv0 + kRows, kFirst);
     }
     if constexpr (RULE) {
       if ((kv0 < seen.all_lo || min(kv0 + kRows, kv_rows) > seen.all_hi) && not_finite<HD, kRows>(vs)) odd = true;

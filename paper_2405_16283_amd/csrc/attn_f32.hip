@@ -23,6 +23,7 @@
 namespace tn {
 namespace {
 
+constexpr int fwd_lds(int hd) { return 4 * (64 * (hd + 4) + hd * (64 + 4)); }
 constexpr int kRows = 64;  // rows of a workgroup's own side, and rows of the other side per round
 
 constexpr int kPieces(int hd) { return kRows * hd / 4 / 256; }  // pieces of four elements per thread and chunk
@@ -37,16 +38,16 @@ __device__ __forceinline__ void load_chunk(const Side<T, HD>& s, bool transposed
   const T* base = plain ? (const T*)s.t[rt0 * s.nc + s.ct] + (size_t)rin0 * s.tc + s.cin : nullptr;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int p = (I0 + i) * 256 + threadIdx.x, r = p / (HD / 4), c = (p % (HD / 4)) * 4;
+    const int p = (I0 + i) * 256 + (threadIdx.x & 255), r = p / (HD / 4), c = (p % (HD / 4)) * 4;
     v[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    if (r < n) v[i] = plain ? ld4(base + (size_t)r * s.tc + c) : transposed ? s.at_t(row0 + r, c) : s.at(row0 + r, c);
+    if (r < n) v[i] = plain ? ld4_global(base + (size_t)r * s.tc + c) : transposed ? s.at_t(row0 + r, c) : s.at(row0 + r, c);
   }
 }
 template <int HD, int I0 = 0, int N = kPieces(HD)>
 __device__ __forceinline__ void store_chunk(float (*buf)[HD + 4], const f32x4 (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int p = (I0 + i) * 256 + threadIdx.x;
+    const int p = (I0 + i) * 256 + (threadIdx.x & 255);
     *(f32x4*)&buf[p / (HD / 4)][(p % (HD / 4)) * 4] = v[i];
   }
 }
@@ -61,19 +62,19 @@ __device__ __forceinline__ void load_chunk_vt(const Side<T, HD>& s, bool transpo
   const T* base = linear ? (const T*)s.t[rt0 * s.nc + s.ct] + (size_t)s.cin * pitch + rin0 : nullptr;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int p = (I0 + i) * 256 + threadIdx.x, c = p / 16, k = (p % 16) * 4;
+    const int p = (I0 + i) * 256 + (threadIdx.x & 255), c = p / 16, k = (p % 16) * 4;
     v[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     if (plain) {  // n is a multiple of 4 here: the tile's rows are
-      if (k < n) v[i] = ld4(base + (size_t)c * pitch + k);
+      if (k < n) v[i] = ld4_global(base + (size_t)c * pitch + k);
     } else if (linear) {  // (347 keys: with the tile looked up for every element 132 us a launch, so 103)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (k + e < n) v[i][e] = ld(base + (size_t)c * pitch + k + e);
+        if (k + e < n) v[i][e] = ld_global(base + (size_t)c * pitch + k + e);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (k + e < n)
-          v[i][e] = ld(transposed ? tile_elem_t<T>(s.t, s.nc, s.trows, s.tc, s.rows, row0 + k + e, s.c0 + c)
+          v[i][e] = ld_global(transposed ? tile_elem_t<T>(s.t, s.nc, s.trows, s.tc, s.rows, row0 + k + e, s.c0 + c)
                                   : tile_elem<T>(s.t, s.nc, s.trows, s.tc, row0 + k + e, s.c0 + c));
     }
   }
@@ -83,7 +84,7 @@ template <int HD, int I0 = 0, int N = kPieces(HD)>
 __device__ __forceinline__ void store_chunk_vt(float (*buf)[kRows + 4], const f32x4 (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int p = (I0 + i) * 256 + threadIdx.x;
+    const int p = (I0 + i) * 256 + (threadIdx.x & 255);
     *(f32x4*)&buf[p / 16][(p % 16) * 4] = v[i];
   }
 }
@@ -94,7 +95,7 @@ template <int HD, int I0 = 0, int N = kPieces(HD)>
 __device__ __forceinline__ void store_chunk_turned(float (*buf)[kRows + 4], const f32x4 (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int p = (I0 + i) * 256 + threadIdx.x;
+    const int p = (I0 + i) * 256 + (threadIdx.x & 255);
 #pragma unroll
     for (int e = 0; e < 4; ++e) buf[p % (HD / 4) * 4 + e][p / (HD / 4)] = v[i][e];
   }
@@ -110,7 +111,7 @@ __device__ __forceinline__ bool not_finite(const float (*buf)[PITCH]) {
   float z = 0.f;
 #pragma unroll
   for (int i = 0; i < ROWS * COLS / 4 / 256; ++i) {
-    const int p = i * 256 + threadIdx.x;
+    const int p = i * 256 + (threadIdx.x & 255);
     const f32x4 v = *(const f32x4*)&buf[p / (COLS / 4)][p % (COLS / 4) * 4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) z = fmaf(v[e], 0.f, z);
@@ -125,7 +126,9 @@ __device__ __forceinline__ bool any_wave(bool mine, char* lds) {
   __syncthreads();
   if ((threadIdx.x & 63) == 0) said[threadIdx.x >> 6] = wave;
   __syncthreads();
-  return __builtin_expect((said[0] | said[1] | said[2] | said[3]) != 0, 0);
+  int any = 0;
+  for (int w = 0; w < (int)blockDim.x >> 6; ++w) any |= said[w];
+  return __builtin_expect(any != 0, 0);
 }
 
 // What the rows of a workgroup see together, of per-lane ranges (all lanes of the workgroup, lo == hi for nothing): keys before `begin` and from
@@ -141,7 +144,7 @@ __device__ __forceinline__ Seen seen_by_all(int lo, int hi, bool exists, int* ld
     for (int k = 0; k < 4; ++k) v[k] = min(v[k], __shfl_xor(v[k], off, 64));
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) lds[(threadIdx.x >> 6) * 4 + k] = v[k];
+    for (int k = 0; k < 4; ++k) lds[((threadIdx.x & 255) >> 6) * 4 + k] = v[k];  // (both halves find the same)
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < 4; ++w)
@@ -152,9 +155,11 @@ __device__ __forceinline__ Seen seen_by_all(int lo, int hi, bool exists, int* ld
 }
 
 // aux: [rows per Q tile, rows per K/V tile, columns per tile, q rows, kv rows]
-// RULE: scores go by a rule or rows are finished (attn_rule.h); the rest of aux is read.
+// RULE: scores go by a rule or rows are finished (attn_rule.h); the rest of aux is read.  Then two halves of four wavefronts take
+// alternate chunks and are joined at the end: a launch of few workgroups waits for its longest walk over the keys, and one of many
+// has the same eight wavefronts to a compute unit (1024 positions of 16 heads of 64, 256 workgroups, 100 us without, TIME with).
 template <typename T, int HD, bool RULE>
-__global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch b) {
+__global__ void __launch_bounds__(RULE ? 512 : 256, 2) attn_f32_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
   const int* ax = t.aux + d.aux0;
@@ -162,7 +167,8 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   const int nc = d.p.n_col_tiles, gw = nc * tc, hpg = gw / HD;
   const int qblocks = (q_rows + kRows - 1) / kRows;
   const int h = blockIdx.x / qblocks, qb = blockIdx.x % qblocks;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, w = (threadIdx.x & 255) >> 6, n = lane & 15, g = lane >> 4;
+  const int half = RULE ? threadIdx.x >> 8 : 0;
   void* const* Qt = t.ptrs + d.ptr0;
   void* const* Kt = Qt + d.p.n_q_tiles * nc;
   void* const* Vt = Kt + d.p.n_kv_tiles * nc;
@@ -171,8 +177,9 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   const int causal = d.p.causal, k_pos0 = d.p.k_pos0;
 
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  float(*const ks)[HD + 4] = (float(*)[HD + 4])lds;                                   // K chunk [64][HD], padded
-  float(*const vs)[kRows + 4] = (float(*)[kRows + 4])(lds + sizeof(float) * kRows * (HD + 4));  // V^T chunk [HD][64], padded
+  char* const mine = lds + half * fwd_lds(HD);
+  float(*const ks)[HD + 4] = (float(*)[HD + 4])mine;                                   // K chunk [64][HD], padded
+  float(*const vs)[kRows + 4] = (float(*)[kRows + 4])(mine + sizeof(float) * kRows * (HD + 4));  // V^T chunk [HD][64], padded
   bool odd = false;  // a chunk on the diagonal whose V is not finite
 
   const int row = qb * kRows + w * 16 + n, qpos = d.p.q_pos0 + row;
@@ -215,28 +222,34 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
   };
   constexpr std::integral_constant<int, 0> kFirst{};
   constexpr std::integral_constant<int, P> kRest{};
-  if (kAhead && end > begin) {
-    load_chunk<T, HD, 0, P>(K, false, begin, kn);
-    load_v(begin, kFirst);
+  constexpr int kStep = RULE ? 2 * kRows : kRows;
+  const int from = begin + half * kRows;
+  if (kAhead && end > from) {
+    load_chunk<T, HD, 0, P>(K, false, from, kn);
+    load_v(from, kFirst);
   }
-  for (int kv0 = begin; kv0 < end; kv0 += kRows) {
+  for (int kv0 = from; kv0 - half * kRows < end; kv0 += kStep) {
+    const bool there = !RULE || kv0 < end;  // the second half may have no last chunk
     __syncthreads();  // everybody is done with the chunk before
-    if constexpr (!kAhead) {
-      load_chunk<T, HD, 0, P>(K, false, kv0, kn);
-      load_v(kv0, kFirst);
-    }
-    store_chunk<HD, 0, P>(ks, kn);
-    store_v(kFirst);
-    if constexpr (!kAhead) {
-      load_chunk<T, HD, P, P>(K, false, kv0, kn);
-      load_v(kv0, kRest);
-      store_chunk<HD, P, P>(ks, kn);
-      store_v(kRest);
+    if (there) {
+      if constexpr (!kAhead) {
+        load_chunk<T, HD, 0, P>(K, false, kv0, kn);
+        load_v(kv0, kFirst);
+      }
+      store_chunk<HD, 0, P>(ks, kn);
+      store_v(kFirst);
+      if constexpr (!kAhead) {
+        load_chunk<T, HD, P, P>(K, false, kv0, kn);
+        load_v(kv0, kRest);
+        store_chunk<HD, P, P>(ks, kn);
+        store_v(kRest);
+      }
     }
     __syncthreads();
-    if (kAhead && kv0 + kRows < end) {
-      load_chunk<T, HD, 0, P>(K, false, kv0 + kRows, kn);
-      load_v(kv0 + kRows, kFirst);
+    if (!there) continue;
+    if (kAhead && kv0 + kStep < end) {
+      load_chunk<T, HD, 0, P>(K, false, kv0 + kStep, kn);
+      load_v(kv0 + kStep, kFirst);
     }
     if constexpr (RULE) {
       if ((kv0 < seen.all_lo || min(kv0 + kRows, kv_rows) > seen.all_hi) && not_finite<HD, kRows>(vs)) odd = true;
@@ -316,9 +329,28 @@ __global__ void __launch_bounds__(256, 2) attn_f32_kernel(DeviceTables t, Batch 
         if (j & 4) __builtin_amdgcn_sched_barrier(0);
       }
   }
-  if ((causal || RULE) && any_wave(odd, lds)) return attn_by_rows<T, HD, RULE>(t, d, h, qb * kRows, (qb + 1) * kRows, threadIdx.x >> 4, 16);
+  if ((causal || RULE) && any_wave(odd, lds)) return attn_by_rows<T, HD, RULE>(t, d, h, qb * kRows, (qb + 1) * kRows, threadIdx.x >> 4, blockDim.x >> 4);
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  if constexpr (RULE) {  // the second half's state by way of LDS (any_wave has seen to it that the chunks are done with)
+    f32x4* const theirs = (f32x4*)lds;
+    float* const stats = (float*)(lds + 4 * 64 * (HD / 16) * 16);
+    __syncthreads();
+    if (half) {
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) theirs[(w * (HD / 16) + j) * 64 + lane] = o[j];
+      stats[w * 64 + lane] = m;
+      stats[256 + w * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (half) return;
+    const float m2 = stats[w * 64 + lane], l2 = stats[256 + w * 64 + lane];
+    const float mn = fmaxf(m, m2), ms = mn == -INFINITY ? 0.f : mn, w1 = __expf(m - ms), w2 = __expf(m2 - ms);
+    m = mn;
+    l = l * w1 + l2 * w2;
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) o[j] = o[j] * w1 + theirs[(w * (HD / 16) + j) * 64 + lane] * w2;
+  }
   if (row >= q_rows) return;
   if constexpr (RULE)
     if (ax[kRuleFinish]) {
@@ -367,7 +399,7 @@ __device__ __forceinline__ void attn_bwd_f32_body(const DeviceTables& t, const O
   const float scale = d.p.scale;
   auto stat = [&](int r, int which) -> float {  // which 0: lse, 1: D
     const int rt = r / tq;
-    return ((const float*)St[rt])[(size_t)(r - rt * tq) * (2 * hpg) + which * hpg + h];
+    return get_global((const float*)St[rt] + (size_t)(r - rt * tq) * (2 * hpg) + which * hpg + h);
   };
   float(*const x1)[HD + 4] = (float(*)[HD + 4])lds;                                             // K, or Q
   float(*const x2)[HD + 4] = (float(*)[HD + 4])(lds + sizeof(float) * kRows * (HD + 4));        // V, or dO
@@ -547,15 +579,15 @@ __global__ void __launch_bounds__(256, 2) attn_bwd_f32_kernel(DeviceTables t, Ba
   }
 }
 
-constexpr int fwd_lds(int hd) { return 4 * (kRows * (hd + 4) + hd * (kRows + 4)); }
+constexpr int fwd_rule_lds(int hd) { return 2 * fwd_lds(hd); }
 constexpr int bwd_lds(int hd) { return 4 * (2 * kRows * (hd + 4) + 2 * kRows); }
 constexpr int bwd_rule_lds(int hd) { return bwd_lds(hd) + 4 * 2 * kRows; }
 
-template <auto kernel>
+template <auto kernel, int THREADS>
 hipError_t launch(int lds, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   if (const hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)max_blocks, (unsigned)b.n), dim3(256), lds, s, t, b);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)max_blocks, (unsigned)b.n), dim3(THREADS), lds, s, t, b);
   return hipGetLastError();
 }
 
@@ -565,13 +597,13 @@ hipError_t launch_attn_f32(bool reverse, bool rule, int dtype, int head_dim, con
                            hipStream_t s) {
   const bool bf = dtype == TN_BF16;
   if (head_dim != 64 && head_dim != 128) return hipErrorInvalidValue;
-#define TN_PICK(kernel, R, lds)                                                                                     \
-  (head_dim == 64 ? (bf ? launch<kernel<bf16_t, 64, R>>(lds(64), t, b, max_blocks, s)                               \
-                        : launch<kernel<float, 64, R>>(lds(64), t, b, max_blocks, s))                               \
-                  : (bf ? launch<kernel<bf16_t, 128, R>>(lds(128), t, b, max_blocks, s)                             \
-                        : launch<kernel<float, 128, R>>(lds(128), t, b, max_blocks, s)))
-  if (rule) return reverse ? TN_PICK(attn_bwd_f32_kernel, true, bwd_rule_lds) : TN_PICK(attn_f32_kernel, true, fwd_lds);
-  return reverse ? TN_PICK(attn_bwd_f32_kernel, false, bwd_lds) : TN_PICK(attn_f32_kernel, false, fwd_lds);
+#define TN_PICK(kernel, R, threads, lds)                                                                                  \
+  (head_dim == 64 ? (bf ? launch<kernel<bf16_t, 64, R>, threads>(lds(64), t, b, max_blocks, s)                            \
+                        : launch<kernel<float, 64, R>, threads>(lds(64), t, b, max_blocks, s))                            \
+                  : (bf ? launch<kernel<bf16_t, 128, R>, threads>(lds(128), t, b, max_blocks, s)                          \
+                        : launch<kernel<float, 128, R>, threads>(lds(128), t, b, max_blocks, s)))
+  if (rule) return reverse ? TN_PICK(attn_bwd_f32_kernel, true, 256, bwd_rule_lds) : TN_PICK(attn_f32_kernel, true, 512, fwd_rule_lds);
+  return reverse ? TN_PICK(attn_bwd_f32_kernel, false, 256, bwd_lds) : TN_PICK(attn_f32_kernel, false, 256, fwd_lds);
 #undef TN_PICK
 }
 

@@ -22,18 +22,18 @@ struct Side {
   __device__ f32x4 at(int row, int c) const {
     if (whole) {
       const int rt = row / trows;
-      return ld4((const T*)t[rt * nc + ct] + (size_t)(row - rt * trows) * tc + cin + c);
+      return ld4_global((const T*)t[rt * nc + ct] + (size_t)(row - rt * trows) * tc + cin + c);
     }
     f32x4 v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = ld(tile_elem<T>(t, nc, trows, tc, row, c0 + c + i));
+    for (int i = 0; i < 4; ++i) v[i] = ld_global(tile_elem<T>(t, nc, trows, tc, row, c0 + c + i));
     return v;
   }
   // the same where the tiles hold the transpose
   __device__ f32x4 at_t(int row, int c) const {
     f32x4 v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = ld(tile_elem_t<T>(t, nc, trows, tc, rows, row, c0 + c + i));
+    for (int i = 0; i < 4; ++i) v[i] = ld_global(tile_elem_t<T>(t, nc, trows, tc, rows, row, c0 + c + i));
     return v;
   }
 };

@@ -40,7 +40,7 @@ struct Rule {
     k_pos0 = d.p.k_pos0;
     causal = d.p.causal;
   }
-  __device__ float slope(int h) const { return slopes ? slopes[h] : 0.f; }
+  __device__ float slope(int h) const { return slopes ? get_global(slopes + h) : 0.f; }
   // The keys of the block that query row `row` (a row that exists) sees: [lo, hi), counted from the block's first; lo == hi == 0 for none.
   __device__ void visible(int row, int& lo, int& hi) const {
     lo = 0;
@@ -48,7 +48,8 @@ struct Rule {
     if (causal) hi = min(hi, q_pos0 + row - k_pos0 + 1);
     if (spans) {
       const int rt = row / tq;
-      const int* s = (const int*)spans[rt] + (size_t)(row - rt * tq) * 2;
+      typedef __attribute__((ext_vector_type(2))) int int2_t;
+      const int2_t s = get_global((const int2_t*)spans[rt] + (row - rt * tq));
       // (positions are any integers: clipped to the block before its start is taken off)
       lo = min(max(s[0], k_pos0), k_pos0 + kv_rows) - k_pos0;
       hi = min(hi, min(max(s[1], k_pos0), k_pos0 + kv_rows) - k_pos0);

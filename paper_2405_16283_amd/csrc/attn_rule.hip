@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
   bf16x8 qf[HD / 16];
 #pragma unroll
   for (int s = 0; s < HD / 16; ++s)
-    qf[s] = *(const bf16x8*)tile_elem<bf16_t>(Qp, nc, tq, tc, min(row, q_rows - 1), h * HD + s * 16 + g * 8);
+    qf[s] = get_global((const bf16x8*)tile_elem<bf16_t>(Qp, nc, tq, tc, min(row, q_rows - 1), h * HD + s * 16 + g * 8));
   f32x16 ot[HD / 32];
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i)
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
   const Rule rule(t, d);
   auto stat = [&](int r, int which) -> float {
     const int rt = r / tq;
-    return ((const float*)St[rt])[(size_t)(r - rt * tq) * (2 * hpg) + which * hpg + h];
+    return get_global((const float*)St[rt] + (size_t)(r - rt * tq) * (2 * hpg) + which * hpg + h);
   };
   const float scale2 = d.p.scale * kLog2e, inv_scale = 1.f / d.p.scale;
   const float cap2 = rule.cap * kLog2e, into_tanh = 2.f * kLog2e * d.p.scale * rule.inv_cap;
@@ -392,8 +392,8 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
     const int r = min(row, my_rows - 1);
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s) {
-      mine[s] = *(const bf16x8*)tile_elem<bf16_t>(OWN_Q ? Qt : Kt, nc, my_trows, tc, r, h * HD + s * 16 + g * 8);
-      if (MODE != 3) mine2[s] = *(const bf16x8*)tile_elem<bf16_t>(OWN_Q ? Dt : Vt, nc, my_trows, tc, r, h * HD + s * 16 + g * 8);
+      mine[s] = get_global((const bf16x8*)tile_elem<bf16_t>(OWN_Q ? Qt : Kt, nc, my_trows, tc, r, h * HD + s * 16 + g * 8));
+      if (MODE != 3) mine2[s] = get_global((const bf16x8*)tile_elem<bf16_t>(OWN_Q ? Dt : Vt, nc, my_trows, tc, r, h * HD + s * 16 + g * 8));
     }
   }
   const float my_start = OWN_Q ? start(stat(min(row, q_rows - 1), 0)) : 0.f, my_D = OWN_Q ? -stat(min(row, q_rows - 1), 1) : 0.f;

@@ -37,6 +37,16 @@ __device__ __forceinline__ f32x4 ld4(const bf16_t* p) {
   return (f32x4){__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
                  __uint_as_float(u.y & 0xFFFF0000u)};
 }
+// the same from what is known to lie in global memory
+template <typename T> __device__ __forceinline__ T get_global(const T* p) { return *(const TN_GLOBAL T*)p; }
+__device__ __forceinline__ float ld_global(const float* p) { return get_global(p); }
+__device__ __forceinline__ float ld_global(const bf16_t* p) { return bf2f(get_global(p)); }
+__device__ __forceinline__ f32x4 ld4_global(const float* p) { return get_global((const f32x4*)p); }
+__device__ __forceinline__ f32x4 ld4_global(const bf16_t* p) {
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+  const u32x2 u = get_global((const u32x2*)p);
+  return (f32x4){__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u)};
+}
 template <typename T> __device__ __forceinline__ void st(T* p, float v);
 template <> __device__ __forceinline__ void st<float>(float* p, float v) { *p = v; }
 template <> __device__ __forceinline__ void st<bf16_t>(bf16_t* p, float v) { *p = f2bf(v); }

@@ -223,20 +223,26 @@ __global__ void __launch_bounds__(256) head_gain_kernel(DeviceTables t, Batch b)
 // eight elements as loaded, which may be on their way while the head before them is worked on
 template <typename T>
 struct Raw8 {
-  uint4 w[sizeof(T) / 2];
+  f32x4 w[sizeof(T) / 2];
 };
 template <typename T>
 __device__ __forceinline__ Raw8<T> fetch8(const T* p) {
   Raw8<T> r;
 #pragma unroll
-  for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.w[k] = ((const uint4*)p)[k];
+  for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.w[k] = get_global((const f32x4*)p + k);
   return r;
 }
 template <typename T>
 __device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&v)[8]) {
-  const uint32_t* w = (const uint32_t*)r.w;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = sizeof(T) == 4 ? __uint_as_float(w[k]) : __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+  for (int k = 0; k < 8; ++k) {
+    if constexpr (sizeof(T) == 4) {
+      v[k] = r.w[k / 4][k % 4];
+    } else {
+      const uint32_t w = __float_as_uint(r.w[0][k / 2]);
+      v[k] = __uint_as_float(k & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+  }
 }
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&v)[8]) { unpack8(fetch8(p), v); }

@@ -27,7 +27,8 @@ struct Rule {
   const float* slopes;    // of the heads of the column group, or null
   void* const* spans;     // one tensor per Q row tile, or null
   int tq, q_pos0, k_pos0, kv_rows, causal;
-  __device__ Rule() : cap(0.f), inv_cap(0.f), slopes(nullptr), spans(nullptr), tq(1), q_pos0(0), k_pos0(0), kv_rows(0), causal(0) {}
+  bool one_tile;          // of queries
+  __device__ Rule() : cap(0.f), inv_cap(0.f), slopes(nullptr), spans(nullptr), tq(1), q_pos0(0), k_pos0(0), kv_rows(0), causal(0), one_tile(true) {}
   __device__ Rule(const DeviceTables& t, const OpDesc& d) {
     const int* ax = t.aux + d.aux0;
     cap = __int_as_float(ax[kRuleCap]);
@@ -39,6 +40,7 @@ struct Rule {
     q_pos0 = d.p.q_pos0;
     k_pos0 = d.p.k_pos0;
     causal = d.p.causal;
+    one_tile = d.p.n_q_tiles == 1;
   }
   __device__ float slope(int h) const { return slopes ? get_global(slopes + h) : 0.f; }
   // The keys of the block that query row `row` (a row that exists) sees: [lo, hi), counted from the block's first; lo == hi == 0 for none.
@@ -47,7 +49,7 @@ struct Rule {
     hi = kv_rows;
     if (causal) hi = min(hi, q_pos0 + row - k_pos0 + 1);
     if (spans) {
-      const int rt = row / tq;
+      const int rt = one_tile ? 0 : row / tq;
       typedef __attribute__((ext_vector_type(2))) int int2_t;
       const int2_t s = get_global((const int2_t*)spans[rt] + (row - rt * tq));
       // (positions are any integers: clipped to the block before its start is taken off)
@@ -55,6 +57,11 @@ struct Rule {
       hi = min(hi, min(max(s[1], k_pos0), k_pos0 + kv_rows) - k_pos0);
     }
     if (lo >= hi) lo = hi = 0;
+  }
+  // The query behind the last whose position lies in the span of query `row`.
+  __device__ int span_end(int row, int q_rows) const {
+    const int rt = one_tile ? 0 : row / tq;
+    return min(max(get_global((const int*)spans[rt] + (size_t)(row - rt * tq) * 2 + 1), q_pos0), q_pos0 + q_rows) - q_pos0;
   }
   // The score by the rule, of z = scale * q.k; th: tanh(z / cap), whose square the gradient needs
   __device__ float score(float z, float slope, int distance, float& th) const {

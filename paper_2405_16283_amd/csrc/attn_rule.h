@@ -4,9 +4,12 @@
 #include "device.h"
 #include "kernels.h"
 
+#include <climits>
+
 namespace tn {
 namespace {
 
+typedef __attribute__((ext_vector_type(2))) int int2_t;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // tanh to a few units in the last place: for small arguments its series up to x^13 (the next term is below 2^-23 of the sum at
@@ -45,17 +48,18 @@ struct Rule {
   __device__ float slope(int h) const { return slopes ? get_global(slopes + h) : 0.f; }
   // The keys of the block that query row `row` (a row that exists) sees: [lo, hi), counted from the block's first; lo == hi == 0 for none.
   __device__ void visible(int row, int& lo, int& hi) const {
-    lo = 0;
-    hi = kv_rows;
-    if (causal) hi = min(hi, q_pos0 + row - k_pos0 + 1);
+    int2_t span = {INT_MIN, INT_MAX};
     if (spans) {
       const int rt = one_tile ? 0 : row / tq;
-      typedef __attribute__((ext_vector_type(2))) int int2_t;
-      const int2_t s = get_global((const int2_t*)spans[rt] + (row - rt * tq));
-      // (positions are any integers: clipped to the block before its start is taken off)
-      lo = min(max(s[0], k_pos0), k_pos0 + kv_rows) - k_pos0;
-      hi = min(hi, min(max(s[1], k_pos0), k_pos0 + kv_rows) - k_pos0);
+      span = get_global((const int2_t*)spans[rt] + (row - rt * tq));
     }
+    clip(row, span, lo, hi);
+  }
+  // The same of its span.  (Positions are any integers: clipped to the block before its start is taken off.)
+  __device__ void clip(int row, int2_t span, int& lo, int& hi) const {
+    lo = min(max(span.x, k_pos0), k_pos0 + kv_rows) - k_pos0;
+    hi = min(max(span.y, k_pos0), k_pos0 + kv_rows) - k_pos0;
+    if (causal) hi = min(hi, q_pos0 + row - k_pos0 + 1);
     if (lo >= hi) lo = hi = 0;
   }
   // The query behind the last whose position lies in the span of query `row`.

@@ -545,21 +545,18 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
       constexpr int slab = 32 * (HD * 2);
       f32x16 s[SUBS], dp[SUBS];
       // register r of slab u: row os + 32 u + 16 (r >> 3) + 8 g + (r & 7) of the other side
-      float starts[SUBS][16];
+      auto stat4 = [&](int which, float own, int u, int r) -> f32x4 {
+        if (OWN_Q) return (f32x4){own, own, own, own};
+        return *(const f32x4*)(st + which * CH + (sub0 + u) * 32 + 16 * (r >> 3) + 8 * g + (r & 7));
+      };
 #pragma unroll
       for (int u = 0; u < SUBS; ++u)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-          f32x4 v = {my_start, my_start, my_start, my_start}, vd = {my_D, my_D, my_D, my_D};
-          if (!OWN_Q) {
-            const int at = (sub0 + u) * 32 + 16 * (r >> 3) + 8 * g + (r & 7);
-            v = *(const f32x4*)(st + at);
-            if (MODE == 2) vd = *(const f32x4*)(st + CH + at);
-          }
+          const f32x4 v = CAP || SLOPES ? (f32x4){0.f, 0.f, 0.f, 0.f} : stat4(0, my_start, u, r), vd = MODE == 3 ? v : stat4(1, my_D, u, r);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            starts[u][r + e] = v[e];
-            s[u][r + e] = CAP || SLOPES ? 0.f : v[e];
+            s[u][r + e] = v[e];
             dp[u][r + e] = vd[e];
           }
         }
@@ -573,16 +570,18 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
         }
       const float base = from_me + (OWN_Q ? -(float)(os + 8 * g) : (float)(os + 8 * g));
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u)
+      for (int u = 0; u < SUBS; ++u) {
+        f32x4 starts;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
+          if ((CAP || SLOPES) && r % 4 == 0) starts = stat4(0, my_start, u, r);
           const int c = 32 * u + 16 * (r >> 3) + (r & 7);
           float x, y = 0.f;
           if (CAP) {
             y = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[u][r] * into_tanh) + 1.f);
-            x = __builtin_fmaf(-2.f * cap2, y, starts[u][r]);
+            x = __builtin_fmaf(-2.f * cap2, y, starts[r % 4]);
           } else {
-            x = SLOPES ? __builtin_fmaf(s[u][r], scale2, starts[u][r]) : s[u][r] * scale2;
+            x = SLOPES ? __builtin_fmaf(s[u][r], scale2, starts[r % 4]) : s[u][r] * scale2;
           }
           if (SLOPES) x = __builtin_fmaf(-slope2, fabsf(base + (OWN_Q ? -(float)c : (float)c)), x);
           float p = __builtin_amdgcn_exp2f(x);
@@ -590,6 +589,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
           if (CAP && MODE != 3) p *= __builtin_fmaf(-y, y, y);
           s[u][r] = p;
         }
+      }
       if (!all_see) {  // (the empty statement: a branch, not selects on every slab)
         if (OWN_Q) {
           int first = lo - os - 8 * g;

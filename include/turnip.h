@@ -375,6 +375,26 @@ typedef struct {
    * two products per layer and the W1 and W3 tiles a second time, keeping them under a cap costs their way to
    * the host and back.  Layers that are checkpointed as a whole are not affected. */
   int32_t recompute_gate_up;
+  /* Heads of queries and keys (the fields of TN_OP_HEAD_ROPE; all 0: TN_OP_ROPE).  Any of them set needs tile to be
+   * a multiple of head_dim.  qk_norm != 0: each query and key head is normalised (eps) and multiplied by a gain of the layer
+   * (inputs TN_T_GQ, TN_T_GK, [1, head_dim]; frozen under train, like the other gains) before it is rotated.
+   * row_positions != 0: rows take their positions from TN_T_POS (TN_I32, [rows, 1]) instead of their place in the sequence. */
+  int32_t qk_norm;
+  int32_t rope_half;
+  int32_t rotary_dim;
+  float rope_factor;
+  float rope_low;
+  float rope_high;
+  int32_t rope_len0;
+  int32_t row_positions;
+  /* The score rule of all attention vertices (see ATTN_BLOCK; not with materialize_scores).  score_slopes != 0: one slope per
+   * head, TN_T_SLOPES (fp32, [1, n_heads]).  score_spans 1: every row's span of keys, TN_T_SPANS (TN_I32, [rows, 2], positions in the row's
+   * sequence), on top of the causal mask; 2: instead of it -- every query block then meets every key block, and the keys of a
+   * sequence are formed before its first attention vertex (not with decode_steps).  V is read as plain tiles at
+   * full speed: v_transposed == 0 (bf16). */
+  float score_cap;
+  int32_t score_slopes;
+  int32_t score_spans;
 } tn_llama_config;
 
 /* Which vertex is which piece of which tensor of the decoder. */
@@ -383,7 +403,8 @@ enum {
   TN_T_Y, TN_T_K, TN_T_V,
   TN_T_AQ, TN_T_BQ, TN_T_AV, TN_T_BV, TN_T_PROBE,          /* adapter matrices and the probe (inputs)      */
   TN_T_DAQ, TN_T_DBQ, TN_T_DAV, TN_T_DBV, TN_T_DX,           /* their gradients and that of x (outputs)      */
-  TN_T_H                                                     /* hidden state after a layer (hidden_outputs)  */
+  TN_T_H,                                                    /* hidden state after a layer (hidden_outputs)  */
+  TN_T_GQ, TN_T_GK, TN_T_POS, TN_T_SPANS, TN_T_SLOPES        /* qk_norm, row_positions, the score rule (inputs) */
 };
 typedef struct {
   tn_vid vid;

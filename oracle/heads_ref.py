@@ -116,3 +116,53 @@ def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, s
                                     ("dv", (e_p + products * p).T @ dO.abs(), u * rows * (p.T @ dO.abs()), p.T @ dO)):
             out[name].append(err + mag + storage * (val.abs() + err + mag) + tiny)
     return {k_: torch.stack(x, 1) if k_ == "lse" else torch.cat(x, 1) for k_, x in out.items() if x}
+
+
+def decoder(cfg, w, heads, probe=None, storage=None):
+    """The decoder of lora_ref (float64 arrays by name in `w`: weights, x, adapters where there are any) with the tiler's options on heads
+    and scores: `heads` as the harness takes it, its inputs in `w` too (gq.l, gk.l, positions, spans, slopes).  Returns y, and with `probe`
+    the gradients of sum(y * probe) by the adapters and x.  storage "bf16": every tensor that the layer stores, and the gradient arriving at
+    it, rounded to bf16 (lora_ref's model of a bf16 pipeline): how far from the exact result a correct one may stand."""
+    from oracle.lora_ref import _Stored
+    S = _Stored.apply if storage == "bf16" else (lambda z: z)
+    t = {k: torch.tensor(a, dtype=torch.float64) for k, a in w.items()}
+    wanted = [k for k in t if k.split(".")[0] in ("aq", "bq", "av", "bv")] + ["x"]
+    for k in wanted:
+        t[k].requires_grad_(probe is not None)
+    hd, seq = cfg.head_dim, cfg.total_seq
+    turned = any(heads.get(k) for k in ("qk_norm", "rope_half", "rotary_dim", "row_positions")) or heads.get("rope_factor", 0) > 1
+    freq = frequencies(heads.get("rotary_dim", 0) or hd, float(cfg.rope_base), heads.get("rope_factor", 0.0) if turned else 0.0,
+                       heads.get("rope_len0", 0), heads.get("rope_low", 0.0), heads.get("rope_high", 0.0))
+    scale = 1 / math.sqrt(hd)
+
+    def norm(x, g):
+        return x / torch.sqrt((x * x).mean(-1, keepdim=True) + cfg.eps) * g
+
+    outs = []
+    for b in range(cfg.batch):
+        rows = slice(b * seq, (b + 1) * seq)
+        x = t["x"][rows]
+        pos = t["positions"][rows, 0].detach() if heads.get("row_positions") else torch.arange(seq)
+        spans = w["spans"][rows].astype(int) if heads.get("score_spans") else None
+        ok = visible(seq, seq, 0, 0, heads.get("score_spans", 0) != 2, spans)
+        slopes = t["slopes"].reshape(-1) if heads.get("score_slopes") else None
+        for l in range(cfg.layers):
+            a = S(norm(x, t[f"g1.{l}"]))
+            q, k, v = S(a @ t[f"wq.{l}"]), S(a @ t[f"wk.{l}"]), S(a @ t[f"wv.{l}"])
+            if f"aq.{l}" in t:
+                q = S(q + S(S(a @ t[f"aq.{l}"]) @ t[f"bq.{l}"]))
+                v = S(v + S(S(a @ t[f"av.{l}"]) @ t[f"bv.{l}"]))
+            if heads.get("qk_norm"):
+                q, k = head_norm(q, hd, t[f"gq.{l}"], cfg.eps), head_norm(k, hd, t[f"gk.{l}"], cfg.eps)
+            q, k = (S(head_rotate(z, hd, pos, freq, bool(heads.get("rope_half")))) for z in (q, k))
+            o, _ = attention(q, k, v, hd, scale, ok, heads.get("score_cap", 0.0), slopes)
+            h1 = S(x + S(S(o) @ t[f"wo.{l}"]))
+            bn = S(norm(h1, t[f"g2.{l}"]))
+            gate, up = S(bn @ t[f"w1.{l}"]), S(bn @ t[f"w3.{l}"])
+            x = S(h1 + S(S(gate * torch.sigmoid(gate) * up) @ t[f"w2.{l}"]))
+        outs.append(x)
+    y = torch.cat(outs)
+    if probe is None:
+        return y.detach().numpy()
+    grads = torch.autograd.grad((y * torch.tensor(probe)).sum(), [t[k] for k in wanted])
+    return y.detach().numpy(), {k: g.numpy() for k, g in zip(wanted, grads)}

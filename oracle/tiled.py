@@ -67,6 +67,8 @@ def round_bf16(x: np.ndarray) -> np.ndarray:
 def round_store(x: np.ndarray, dtype: str) -> np.ndarray:
     if dtype == "bf16":
         return round_bf16(x)
+    if dtype == "i32":  # positions and spans
+        return np.asarray(x, dtype=np.float64)
     return np.asarray(x, dtype=np.float32).astype(np.float64)
 
 
@@ -139,6 +141,28 @@ def _eval_vertex(kind: str, p: dict, ins: Sequence[np.ndarray]) -> np.ndarray:
         y[:, 0::2] = x[:, 0::2] * cs - x[:, 1::2] * sn
         y[:, 1::2] = x[:, 0::2] * sn + x[:, 1::2] * cs
         return y
+    if kind == "head_rope":
+        ins = list(ins)
+        x, hd = ins.pop(0), p["head_dim"]
+        rows = x.shape[0]
+        h = x.reshape(rows, -1, hd)
+        if p.get("norm"):
+            h = h / np.sqrt(np.mean(h * h, axis=-1, keepdims=True) + p["eps"]) * ins.pop(0).reshape(-1)
+        pos = p["pos0"] + (ins.pop(0)[:, 0] if p.get("positions") else np.arange(rows, dtype=np.float64))
+        rd = p.get("rotary_dim") or hd
+        f = p["base"] ** (-np.arange(0, rd, 2) / rd)
+        if p.get("rope_factor", 0) > 1:
+            turns = p["rope_len0"] * f / (2 * np.pi)
+            kept = np.clip((turns - p["rope_low"]) / (p["rope_high"] - p["rope_low"]), 0, 1) if p["rope_len0"] else np.zeros_like(f)
+            f = kept * f + (1 - kept) * f / p["rope_factor"]
+        ang = (-1 if p.get("mode") else 1) * pos[:, None] * f[None, :]
+        cs, sn = np.cos(ang)[:, None], np.sin(ang)[:, None]
+        n = rd // 2
+        a, b = (slice(0, n), slice(n, rd)) if p.get("rope_half") else (slice(0, rd, 2), slice(1, rd, 2))
+        y = h.copy()
+        y[..., a] = h[..., a] * cs - h[..., b] * sn
+        y[..., b] = h[..., a] * sn + h[..., b] * cs
+        return y.reshape(rows, -1)
     if kind == "attn_block":
         nq, nkv, nc, hd = p["n_q_tiles"], p["n_kv_tiles"], p["n_col_tiles"], p["head_dim"]
         def gather(off, nr, transposed=False):
@@ -154,17 +178,30 @@ def _eval_vertex(kind: str, p: dict, ins: Sequence[np.ndarray]) -> np.ndarray:
         out = np.zeros((rows, gw + 2 * hpg))
         qpos = p["q_pos0"] + np.arange(rows)
         kpos = p["k_pos0"] + np.arange(k.shape[0])
+        # the score rule: a cap, slopes per head, spans per row (the operands behind the tiles)
+        rest = list(ins[(nq + 2 * nkv) * nc:])
+        slopes = rest.pop(0)[0] if p.get("slopes") else None
+        spans = np.concatenate(rest, axis=0) if p.get("spans") else None
         for h in range(hpg):
             sl = slice(h * hd, (h + 1) * hd)
             s = (q[:, sl] @ k[:, sl].T) * p["scale"]
+            if p.get("score_cap"):
+                s = p["score_cap"] * np.tanh(s / p["score_cap"])
+            if slopes is not None:
+                s = s - slopes[h] * np.abs(qpos[:, None] - kpos[None, :])
             if p["causal"]:
                 s = np.where(kpos[None, :] > qpos[:, None], -np.inf, s)
+            if spans is not None:
+                s = np.where((kpos[None, :] >= spans[:, :1]) & (kpos[None, :] < spans[:, 1:]), s, -np.inf)
             m = np.max(s, axis=1)
             msafe = np.where(np.isfinite(m), m, 0.0)
             pr = np.exp(s - msafe[:, None])
             out[:, sl] = pr @ v[:, sl]
             out[:, gw + h] = m
             out[:, gw + hpg + h] = np.sum(pr, axis=1)
+        if p.get("finish"):
+            total = np.repeat(out[:, gw + hpg:], hd, axis=1)
+            return out[:, :gw] / np.where(total == 0, 1.0, total)
         return out
     if kind == "attn_combine":
         hd, hpg = p["head_dim"], p["hpg"]
@@ -173,8 +210,15 @@ def _eval_vertex(kind: str, p: dict, ins: Sequence[np.ndarray]) -> np.ndarray:
         m = np.stack([x[r0:r0 + rows, gw:gw + hpg] for x in ins])  # [j, rows, hpg]
         l = np.stack([x[r0:r0 + rows, gw + hpg:gw + 2 * hpg] for x in ins])
         mstar = np.max(m, axis=0)
+        if p.get("finish"):  # a row that no partial has seen a key of
+            mstar = np.where(np.isfinite(mstar), mstar, 0.0)
         w = np.exp(m - mstar[None])  # exp(-inf) = 0 for empty partials
         lstar = np.sum(l * w, axis=0)
+        if p.get("finish") == 2:
+            with np.errstate(divide="ignore"):
+                return mstar + np.log(lstar)
+        if p.get("finish"):
+            lstar = np.where(lstar == 0, 1.0, lstar)
         out = np.zeros((rows, cols))
         head_of_col = (c0 + np.arange(cols)) // hd
         for j, x in enumerate(ins):

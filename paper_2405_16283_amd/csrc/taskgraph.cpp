@@ -373,11 +373,11 @@ struct Tiler {
   }
 
   tn_vid input(int32_t rws, int32_t cls, int32_t residency, int32_t tensor, int32_t layer, Range rr,
-               Range cr) {
+               Range cr, int32_t dtype = -1) {
     Vertex v;
     v.kind = TN_OP_INPUT;
     v.residency = residency;
-    v.desc = {c.dtype, rws, cls};
+    v.desc = {dtype < 0 ? c.dtype : dtype, rws, cls};
     g.v.push_back(v);
     tn_vid id = (tn_vid)g.v.size() - 1;
     g.bindings.push_back({id, tensor, layer, rr.a, rr.b, cr.a, cr.b, 0});
@@ -468,6 +468,57 @@ struct Tiler {
     p.rope_base = c.rope_base;
     p.mode = inverse ? 1 : 0;
     return op(TN_OP_ROPE, p, {x}, {c.dtype, m, n});
+  }
+
+  // the heads of a query or key tile, by TN_OP_HEAD_ROPE where the configuration asks for more than TN_OP_ROPE does
+  bool heads() const { return c.qk_norm || c.rope_half || c.rotary_dim || c.rope_factor > 1.f || c.row_positions; }
+  tn_op_params head_params(int32_t pos0) const {
+    tn_op_params p{};
+    p.pos0 = c.row_positions ? 0 : pos0;
+    p.head_dim = c.head_dim;
+    p.rope_base = c.rope_base;
+    p.rotary_dim = c.rotary_dim;
+    p.rope_half = c.rope_half;
+    p.positions = c.row_positions;
+    p.norm = c.qk_norm;
+    p.eps = c.eps;
+    p.rope_factor = c.rope_factor;
+    p.rope_low = c.rope_low;
+    p.rope_high = c.rope_high;
+    p.rope_len0 = c.rope_len0;
+    return p;
+  }
+  // gain: the layer's for queries or keys (-1 without qk_norm); pos: the rows' positions (-1 without row_positions)
+  tn_vid turned(tn_vid x, tn_vid gain, tn_vid pos, int32_t pos0, int32_t col_start, int32_t m, int32_t n) {
+    if (!heads()) return rope(x, pos0, col_start, m, n);
+    std::vector<tn_vid> in{x};
+    if (gain >= 0) in.push_back(gain);
+    if (pos >= 0) in.push_back(pos);
+    return op(TN_OP_HEAD_ROPE, head_params(pos0), std::move(in), {c.dtype, m, n});
+  }
+  // gradient of x, the operand of `turned`, from that of its result
+  tn_vid turned_back(tn_vid dy, tn_vid x, tn_vid gain, tn_vid pos, int32_t pos0, int32_t col_start, int32_t m, int32_t n) {
+    if (!heads()) return rope(dy, pos0, col_start, m, n, true);
+    tn_op_params p = head_params(pos0);
+    std::vector<tn_vid> in{dy};
+    if (gain >= 0) {
+      in.push_back(x);
+      in.push_back(gain);
+    } else {
+      p.mode = 1;
+    }
+    if (pos >= 0) in.push_back(pos);
+    return op(gain >= 0 ? TN_OP_HEAD_ROPE_BWD : TN_OP_HEAD_ROPE, p, std::move(in), {c.dtype, m, n});
+  }
+
+  // The score rule of an attention vertex over the Q row tiles whose spans are given; its operands are appended to `in`.
+  bool rule() const { return c.score_cap > 0.f || c.score_slopes || c.score_spans; }
+  void add_rule(tn_op_params& p, std::vector<tn_vid>& in, tn_vid slopes, const std::vector<tn_vid>& spans) const {
+    p.score_cap = c.score_cap;
+    p.slopes = c.score_slopes;
+    p.spans = c.score_spans != 0;
+    if (c.score_slopes) in.push_back(slopes);
+    in.insert(in.end(), spans.begin(), spans.end());
   }
 
   // weight tiles in [in, out] layout, for the reverse pass: grid[i][j] = rows rr[i], columns cc[j]
@@ -763,6 +814,14 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
     return fail(TN_ERR_INVALID, "checkpoint_layers needs checkpoint and must not be negative");
   // layers whose forward tensors the reverse pass forms again instead of reading saved ones
   auto recomputed = [&](int l) { return c.checkpoint && (c.checkpoint_layers == 0 || l < c.checkpoint_layers); };
+  if ((c.qk_norm || c.rope_half || c.rotary_dim || c.rope_factor > 1.f || c.row_positions) && c.tile % c.head_dim)
+    return fail(TN_ERR_SHAPE, "qk_norm, row_positions and the forms of the rotation need tile to be a multiple of head_dim");
+  if (!(c.rope_factor == 0.f || c.rope_factor >= 1.f) || !std::isfinite(c.rope_factor)) return fail(TN_ERR_SHAPE, "rope_factor must be 0 or at least 1");
+  if (!(c.score_cap == 0.f || (c.score_cap >= 1e-6f && c.score_cap <= 1e6f))) return fail(TN_ERR_SHAPE, "score_cap must be 0 or lie in 1e-6 .. 1e6");
+  if (c.score_spans < 0 || c.score_spans > 2 || (c.score_spans == 2 && c.decode_steps > 0))
+    return fail(TN_ERR_INVALID, "score_spans must be 0, 1 or 2, and 2 does not go with decode_steps");
+  if ((c.score_cap != 0.f || c.score_slopes || c.score_spans) && c.materialize_scores)
+    return fail(TN_ERR_INVALID, "a score rule does not go with materialize_scores");
   if (c.materialize_scores && (c.tile != c.head_dim || c.train || c.kv_outputs))
     return fail(TN_ERR_INVALID, "materialize_scores needs tile == head_dim and neither train nor kv_outputs");
 
@@ -784,9 +843,34 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
       }
   }
 
+  // positions and spans of the rows of every sequence, slopes of every head group
+  const bool rule = t.rule(), two_sided = c.score_spans == 2;
+  std::vector<std::vector<tn_vid>> pos(c.batch), spans(c.batch);
+  auto row_input = [&](int32_t tensor, Range rr, int32_t cols) {
+    return t.input(rr.len(), cols, c.x_residency, tensor, -1, rr, {0, cols}, TN_I32);
+  };
+  for (int b = 0; b < c.batch; ++b) {
+    pos[b].assign(t.rows.size(), -1);
+    for (size_t i = 0; i < t.rows.size(); ++i) {
+      const Range rr{b * c.seq + t.rows[i].a, b * c.seq + t.rows[i].b};
+      if (c.row_positions) pos[b][i] = row_input(TN_T_POS, rr, 1);
+      if (c.score_spans) spans[b].push_back(row_input(TN_T_SPANS, rr, 2));
+    }
+  }
+  std::vector<tn_vid> slopes(n_groups, -1);
+  for (int32_t gi = 0; c.score_slopes && gi < n_groups; ++gi)
+    slopes[gi] = t.input(1, hpg, c.weights_residency, TN_T_SLOPES, -1, {0, 1}, {gi * hpg, (gi + 1) * hpg}, TN_F32);
+  auto spans_of = [&](int b, const std::vector<size_t>& rt) {
+    std::vector<tn_vid> out;
+    for (size_t i : rt)
+      if (c.score_spans) out.push_back(spans[b][i]);
+    return out;
+  };
+
   // what the reverse pass needs of the forward pass, per layer and sequence, indexed by row tile
   struct Saved {
     Grid xin, a, q, k, v, h1, gate, up;
+    Grid qpre, kpre, o, lse;  // with qk_norm: the rotation's operands; with a score rule: finished attention and log-sum-exps
     std::vector<tn_vid> rstd1, rstd2, tq, tv;
   };
   std::vector<std::vector<Saved>> saved(c.train ? c.layers : 0, std::vector<Saved>(c.batch));
@@ -795,6 +879,7 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
   struct LayerInputs {
     Grid wq, wk, wv, wo, w1, w3, w2;
     std::vector<tn_vid> g1, g2, aq, bq, av, bv, aqT, bqT, avT, bvT;
+    tn_vid gq = -1, gk = -1;
   };
   std::vector<LayerInputs> lin(c.train || c.decode_steps ? c.layers : 0);
   std::vector<Grid> kcache(c.decode_steps ? c.layers : 0), vcache(c.decode_steps ? c.layers : 0);  // K, V of the prefill
@@ -816,14 +901,18 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
     if (sv) {
       sv->xin = xb;
       for (Grid* gp : {&sv->a, &sv->q, &sv->k, &sv->v, &sv->h1, &sv->gate, &sv->up}) gp->assign(t.rows.size(), {});
+      for (Grid* gp : {&sv->qpre, &sv->kpre, &sv->o, &sv->lse}) gp->assign(t.rows.size(), {});
       for (auto* vp : {&sv->rstd1, &sv->rstd2, &sv->tq, &sv->tv}) vp->assign(t.rows.size(), -1);
     }
     Grid kk(t.rows.size()), vv(t.rows.size());  // K, V of the stripes done so far
-    for (size_t s = 0; s < stripes.size(); ++s) {
-      std::vector<size_t> rt;  // row tiles of this stripe
+    Grid q(t.rows.size());
+    auto tiles_of = [&](size_t s) {  // row tiles of a stripe
+      std::vector<size_t> rt;
       for (size_t i = 0; i < t.rows.size(); ++i)
         if (t.rows[i].a >= stripes[s].a && t.rows[i].a < stripes[s].b) rt.push_back(i);
-      Grid q(t.rows.size());
+      return rt;
+    };
+    auto project = [&](const std::vector<size_t>& rt) {
       for (size_t i : rt) {
         const int32_t m = t.rows[i].len();
         tn_vid st1 = -1, tq = -1, tv = -1;
@@ -841,9 +930,14 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
             vj = t.op(TN_OP_ADD, tn_op_params{}, {vj, t.gemm_list({tv}, {bvT[j]}, m, n, false, true, vt)},
                       vt ? tn_tensor_desc{c.dtype, n, m} : tn_tensor_desc{c.dtype, m, n});
           }
-          q[i].push_back(t.rope(qj, t.rows[i].a, t.dcols[j].a, m, n));
-          kk[i].push_back(t.rope(t.gemm(a, wk, j, m, n), t.rows[i].a, t.dcols[j].a, m, n));
+          q[i].push_back(t.turned(qj, w.gq, pos[b][i], t.rows[i].a, t.dcols[j].a, m, n));
+          const tn_vid kj = t.gemm(a, wk, j, m, n);
+          kk[i].push_back(t.turned(kj, w.gk, pos[b][i], t.rows[i].a, t.dcols[j].a, m, n));
           vv[i].push_back(vj);
+          if (sv && c.qk_norm) {
+            sv->qpre[i].push_back(qj);
+            sv->kpre[i].push_back(kj);
+          }
           if (sv && j + 1 == nd) {
             sv->a[i] = a; sv->q[i] = q[i]; sv->k[i] = kk[i]; sv->v[i] = vv[i];
             sv->rstd1[i] = st1; sv->tq[i] = tq; sv->tv[i] = tv;
@@ -860,6 +954,12 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
           }
         }
       }
+    };
+    if (two_sided)
+      for (size_t s = 0; s < stripes.size(); ++s) project(tiles_of(s));
+    for (size_t s = 0; s < stripes.size(); ++s) {
+      const std::vector<size_t> rt = tiles_of(s);
+      if (!two_sided) project(rt);
       // attention of this stripe against stripes 0..s, one partial per pair, per head group
       Grid o(t.rows.size(), std::vector<tn_vid>(nd, -1));
       if (c.materialize_scores) {
@@ -897,7 +997,11 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
         std::vector<tn_vid> parts;
         // attn_whole_rows: one vertex per query block over all keys up to the block's own, instead of one per
         // key block (its online softmax runs over the whole range; one partial instead of s + 1)
-        for (size_t s2 = c.attn_whole_rows ? s : 0; s2 <= s; ++s2) {
+        // (score_spans 2: over all keys there are)
+        const size_t last = two_sided ? stripes.size() - 1 : s;
+        // with a rule a vertex that sees all keys of one row tile leaves finished rows, and no combine is needed
+        const bool finished = rule && c.attn_whole_rows && rt.size() == 1 && ctg == 1;
+        for (size_t s2 = c.attn_whole_rows ? last : 0; s2 <= last; ++s2) {
           const int32_t k_from = c.attn_whole_rows ? 0 : stripes[s2].a;
           std::vector<size_t> kt;
           for (size_t i = 0; i < t.rows.size(); ++i)
@@ -913,20 +1017,37 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
           p.head_dim = c.head_dim;
           p.q_pos0 = stripes[s].a;
           p.k_pos0 = k_from;
-          p.causal = (s2 == s);
+          p.causal = (s2 == s) && !two_sided;
           p.v_trans = c.v_transposed ? 1 : 0;
           p.scale = 1.0f / std::sqrt((float)c.head_dim);
-          parts.push_back(t.op(TN_OP_ATTN_BLOCK, p, std::move(in), {TN_F32, stripes[s].len(), gw + 2 * hpg}));
+          if (rule) t.add_rule(p, in, slopes[gi], spans_of(b, rt));
+          if (finished) {
+            p.finish = 1;
+            o[rt[0]][gi] = t.op(TN_OP_ATTN_BLOCK, p, std::move(in), {c.dtype, t.rows[rt[0]].len(), gw});
+          } else {
+            parts.push_back(t.op(TN_OP_ATTN_BLOCK, p, std::move(in), {TN_F32, stripes[s].len(), gw + 2 * hpg}));
+          }
         }
         for (size_t i : rt)
-          for (int32_t cc = 0; cc < ctg; ++cc) {
+          for (int32_t cc = 0; cc < ctg && !finished; ++cc) {
             tn_op_params p{};
+            p.finish = c.score_spans ? 1 : 0;  // a row may see nothing
             p.row0 = t.rows[i].a - stripes[s].a;
             p.col0 = cc * c.tile;
             p.head_dim = c.head_dim;
             p.hpg = hpg;
             o[i][gi * ctg + cc] = t.op(TN_OP_ATTN_COMBINE, p, parts,
                                       {c.dtype, t.rows[i].len(), t.dcols[gi * ctg + cc].len()});
+          }
+        if (sv && rule)  // (train: a head group is one column tile)
+          for (size_t i : rt) {
+            tn_op_params p{};
+            p.finish = 2;
+            p.row0 = t.rows[i].a - stripes[s].a;
+            p.head_dim = c.head_dim;
+            p.hpg = hpg;
+            sv->lse[i].push_back(t.op(TN_OP_ATTN_COMBINE, p, parts, {TN_F32, t.rows[i].len(), hpg}));
+            sv->o[i].push_back(o[i][gi]);
           }
       }
       // output projection, residual, feed-forward, residual -- row tile by row tile
@@ -992,7 +1113,12 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
       bqT.push_back(t.op(TN_OP_TRANSPOSE, tn_op_params{}, {bq[j]}, {c.dtype, n, rk}));
       bvT.push_back(t.op(TN_OP_TRANSPOSE, tn_op_params{}, {bv[j]}, {c.dtype, n, rk}));
     }
-    const LayerInputs w{wq, wk, wv, wo, w1, w3, w2, g1, g2, aq, bq, av, bv, aqT, bqT, avT, bvT};
+    tn_vid gq = -1, gk = -1;
+    if (c.qk_norm) {
+      gq = t.input(1, c.head_dim, c.weights_residency, TN_T_GQ, l, {0, 1}, {0, c.head_dim});
+      gk = t.input(1, c.head_dim, c.weights_residency, TN_T_GK, l, {0, 1}, {0, c.head_dim});
+    }
+    const LayerInputs w{wq, wk, wv, wo, w1, w3, w2, g1, g2, aq, bq, av, bv, aqT, bqT, avT, bvT, gq, gk};
     if (c.train || c.decode_steps) lin[l] = w;
     for (int b = 0; b < c.batch; ++b) {
       if (recomputed(l)) layer_in[l][b] = x[b];
@@ -1026,14 +1152,17 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
       const Range rr{P + u, P + u + 1};
       std::vector<tn_vid> xr(nd);
       for (size_t j = 0; j < nd; ++j) xr[j] = t.input(1, t.dcols[j].len(), c.x_residency, TN_T_X, -1, rr, t.dcols[j]);
+      const tn_vid at = c.row_positions ? row_input(TN_T_POS, rr, 1) : -1;
+      std::vector<tn_vid> span;
+      if (c.score_spans) span.push_back(row_input(TN_T_SPANS, rr, 2));
       for (int l = 0; l < c.layers; ++l) {
         const LayerInputs& w = lin[l];
         auto a = t.rmsnorm(xr, w.g1, 1);
         std::vector<tn_vid> q(nd), kr(nd), vr(nd);
         for (size_t j = 0; j < nd; ++j) {
           const int32_t n = t.dcols[j].len();
-          q[j] = t.rope(t.gemm(a, w.wq, j, 1, n), P + u, t.dcols[j].a, 1, n);
-          kr[j] = t.rope(t.gemm(a, w.wk, j, 1, n), P + u, t.dcols[j].a, 1, n);
+          q[j] = t.turned(t.gemm(a, w.wq, j, 1, n), w.gq, at, P + u, t.dcols[j].a, 1, n);
+          kr[j] = t.turned(t.gemm(a, w.wk, j, 1, n), w.gk, at, P + u, t.dcols[j].a, 1, n);
           vr[j] = t.gemm(a, w.wv, j, 1, n, c.v_transposed != 0);
           if (c.kv_outputs && layer_is_output(l)) {
             t.mark_output(kr[j], TN_T_K, l, rr, t.dcols[j]);
@@ -1064,6 +1193,7 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
             for (size_t i : kt) for (int32_t cc = 0; cc < ctg; ++cc) in.push_back(vcache[l][i][gi * ctg + cc]);
             p.n_kv_tiles = (int32_t)kt.size();
             p.k_pos0 = stripes[s2].a;
+            if (rule) t.add_rule(p, in, slopes[gi], span);
             parts.push_back(t.op(TN_OP_ATTN_BLOCK, p, std::move(in), {TN_F32, 1, gw + 2 * hpg}));
           }
           {  // the generated positions so far, this row's included: one single-row tile each
@@ -1073,10 +1203,12 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
             for (int v = 0; v <= u; ++v) for (int32_t cc = 0; cc < ctg; ++cc) in.push_back(vdec[l][v][gi * ctg + cc]);
             p.n_kv_tiles = u + 1;
             p.k_pos0 = P;
+            if (rule) t.add_rule(p, in, slopes[gi], span);
             parts.push_back(t.op(TN_OP_ATTN_BLOCK, p, std::move(in), {TN_F32, 1, gw + 2 * hpg}));
           }
           for (int32_t cc = 0; cc < ctg; ++cc) {
             tn_op_params pc{};
+            pc.finish = c.score_spans ? 1 : 0;
             pc.row0 = 0;
             pc.col0 = cc * c.tile;
             pc.head_dim = c.head_dim;
@@ -1197,11 +1329,53 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
           for (size_t i = 0; i < nr; ++i) {
             const int32_t m = t.rows[i].len();
             vn[i] = c.v_transposed ? transposed(sv.v[i][j], n, m) : sv.v[i][j];
+            if (rule) continue;  // its kernels read plain tiles
             kT[i] = transposed(sv.k[i][j], m, n);
             qT[i] = transposed(sv.q[i][j], m, n);
             dOT[i] = transposed(dO[i][j], m, n);
           }
-          for (size_t i = 0; i < nr; ++i) {  // query tile i against the key tiles 0..i
+          for (size_t i = 0; rule && i < nr; ++i) {  // query tile i against the key tiles it may see
+            const size_t to = two_sided ? nr : i + 1;
+            const int32_t m = t.rows[i].len();
+            tn_op_params ps{};
+            ps.mode = 4;
+            ps.n_q_tiles = ps.n_col_tiles = 1;
+            ps.head_dim = c.head_dim;
+            stats[i] = t.op(TN_OP_ATTN_BWD, ps, {sv.o[i][j], dO[i][j], sv.lse[i][j]}, {TN_F32, m, 2 * hpg_});
+            std::vector<tn_vid> in{sv.q[i][j]};
+            for (size_t r = 0; r < to; ++r) in.push_back(sv.k[r][j]);
+            for (size_t r = 0; r < to; ++r) in.push_back(vn[r]);
+            in.push_back(dO[i][j]);
+            in.push_back(stats[i]);
+            p.n_q_tiles = 1;
+            p.n_kv_tiles = (int32_t)to;
+            p.q_pos0 = t.rows[i].a;
+            p.k_pos0 = 0;
+            p.mode = 1;
+            p.causal = !two_sided;
+            t.add_rule(p, in, slopes[j], spans_of(b, {i}));
+            dq[i][j] = t.op(TN_OP_ATTN_BWD, p, std::move(in), {c.dtype, m, n});
+          }
+          for (size_t r = 0; rule && r < nr; ++r) {  // key tile r against the query tiles that may see it
+            std::vector<size_t> qt;
+            for (size_t i = two_sided ? 0 : r; i < nr; ++i) qt.push_back(i);
+            std::vector<tn_vid> in;
+            for (size_t i : qt) in.push_back(sv.q[i][j]);
+            in.push_back(sv.k[r][j]);
+            in.push_back(vn[r]);
+            for (size_t i : qt) in.push_back(dO[i][j]);
+            for (size_t i : qt) in.push_back(stats[i]);
+            p.n_q_tiles = (int32_t)qt.size();
+            p.n_kv_tiles = 1;
+            p.q_pos0 = t.rows[qt[0]].a;
+            p.k_pos0 = t.rows[r].a;
+            t.add_rule(p, in, slopes[j], spans_of(b, qt));
+            p.mode = 2;
+            dk[r][j] = t.op(TN_OP_ATTN_BWD, p, in, {c.dtype, t.rows[r].len(), n});
+            p.mode = 3;
+            dv[r][j] = t.op(TN_OP_ATTN_BWD, p, std::move(in), {c.dtype, t.rows[r].len(), n});
+          }
+          for (size_t i = 0; !rule && i < nr; ++i) {  // query tile i against the key tiles 0..i
             std::vector<tn_vid> in{sv.q[i][j]};
             for (size_t r = 0; r <= i; ++r) in.push_back(sv.k[r][j]);
             for (size_t r = 0; r <= i; ++r) in.push_back(vn[r]);
@@ -1219,7 +1393,7 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
             p.trans_a = 1;
             dq[i][j] = t.op(TN_OP_ATTN_BWD, p, std::move(in), {c.dtype, t.rows[i].len(), n});
           }
-          for (size_t r = 0; r < nr; ++r) {  // key tile r against the query tiles r..end
+          for (size_t r = 0; !rule && r < nr; ++r) {  // key tile r against the query tiles r..end
             std::vector<tn_vid> in;
             for (size_t i = r; i < nr; ++i) in.push_back(sv.q[i][j]);
             in.push_back(sv.k[r][j]);
@@ -1245,8 +1419,9 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
           const int32_t m = t.rows[i].len();
           std::vector<tn_vid> big;  // dq, dk (before the rotation), dv: operands of the gradient of a
           for (size_t j = 0; j < nd; ++j) {
-            dq[i][j] = t.rope(dq[i][j], t.rows[i].a, t.dcols[j].a, m, t.dcols[j].len(), true);
-            dk[i][j] = t.rope(dk[i][j], t.rows[i].a, t.dcols[j].a, m, t.dcols[j].len(), true);
+            const int32_t n = t.dcols[j].len();
+            dq[i][j] = t.turned_back(dq[i][j], c.qk_norm ? sv.qpre[i][j] : -1, w.gq, pos[b][i], t.rows[i].a, t.dcols[j].a, m, n);
+            dk[i][j] = t.turned_back(dk[i][j], c.qk_norm ? sv.kpre[i][j] : -1, w.gk, pos[b][i], t.rows[i].a, t.dcols[j].a, m, n);
           }
           big = dq[i];
           big.insert(big.end(), dk[i].begin(), dk[i].end());

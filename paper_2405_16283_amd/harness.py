@@ -13,14 +13,17 @@ _TENSOR_NAMES = {B.TN_T_X: "x", B.TN_T_WQ: "wq", B.TN_T_WK: "wk", B.TN_T_WV: "wv
                  B.TN_T_W1: "w1", B.TN_T_W3: "w3", B.TN_T_W2: "w2", B.TN_T_G1: "g1", B.TN_T_G2: "g2",
                  B.TN_T_Y: "y", B.TN_T_K: "k", B.TN_T_V: "v", B.TN_T_AQ: "aq", B.TN_T_BQ: "bq", B.TN_T_AV: "av",
                  B.TN_T_BV: "bv", B.TN_T_PROBE: "probe", B.TN_T_DAQ: "daq", B.TN_T_DBQ: "dbq", B.TN_T_DAV: "dav",
-                 B.TN_T_DBV: "dbv", B.TN_T_DX: "dx", B.TN_T_H: "h"}
+                 B.TN_T_DBV: "dbv", B.TN_T_DX: "dx", B.TN_T_H: "h", B.TN_T_GQ: "gq", B.TN_T_GK: "gk", B.TN_T_POS: "positions",
+                 B.TN_T_SPANS: "spans", B.TN_T_SLOPES: "slopes"}
 OUTPUT_TENSORS = ("y", "k", "v", "daq", "dbq", "dav", "dbv", "dx", "h")
 OP_NAMES = {B.TN_OP_INPUT: "input", B.TN_OP_GEMM: "gemm", B.TN_OP_RMS_STAT: "rms_stat",
             B.TN_OP_RMS_APPLY: "rms_apply", B.TN_OP_ROPE: "rope", B.TN_OP_ATTN_BLOCK: "attn_block",
             B.TN_OP_ATTN_COMBINE: "attn_combine", B.TN_OP_SILU_MUL: "silu_mul", B.TN_OP_ADD: "add",
             B.TN_OP_SILU_MUL_BWD: "silu_mul_bwd", B.TN_OP_RMS_BWD_STAT: "rms_bwd_stat",
             B.TN_OP_RMS_BWD_APPLY: "rms_bwd_apply", B.TN_OP_ATTN_BWD: "attn_bwd", B.TN_OP_TRANSPOSE: "transpose",
-            B.TN_OP_SUM: "sum", B.TN_OP_SOFTMAX_STAT: "softmax_stat", B.TN_OP_SOFTMAX_APPLY: "softmax_apply"}
+            B.TN_OP_SUM: "sum", B.TN_OP_SOFTMAX_STAT: "softmax_stat", B.TN_OP_SOFTMAX_APPLY: "softmax_apply",
+            B.TN_OP_HEAD_ROPE: "head_rope", B.TN_OP_HEAD_ROPE_BWD: "head_rope_bwd", B.TN_OP_COL_SUM: "col_sum"}
+_DTYPE_NAMES = {B.TN_F32: "f32", B.TN_BF16: "bf16", B.TN_I32: "i32"}
 MG_KIND_NAMES = {B.TN_MG_INPUT: "input", B.TN_MG_LOAD: "load", B.TN_MG_OP: "op", B.TN_MG_OFFLOAD: "offload",
                  B.TN_MG_RELOAD: "reload", B.TN_MG_DROP: "drop", B.TN_MG_STORE: "store", B.TN_MG_JOIN: "join"}
 EDGE_NAMES = {B.TN_EDGE_DATA: "data", B.TN_EDGE_MEM: "mem", B.TN_EDGE_ORDER: "order"}
@@ -32,8 +35,10 @@ def llama_config_struct(cfg, kv_outputs: bool = False, weights_transposed: bool 
                         checkpoint: bool = False, hidden_outputs: bool = False,
                         output_layer_stride: int = 0, attn_whole_rows: bool = False,
                         checkpoint_layers: int = 0, fuse_epilogues: int = 0,
-                        recompute_normed: bool = False, recompute_gate_up: bool = False) -> B.tn_llama_config:
-    """workloads.LlamaConfig -> tn_llama_config."""
+                        recompute_normed: bool = False, recompute_gate_up: bool = False,
+                        heads: Optional[dict] = None) -> B.tn_llama_config:
+    """workloads.LlamaConfig -> tn_llama_config.  heads: the fields of tn_llama_config on heads and scores (qk_norm, rope_half,
+    rotary_dim, rope_factor, rope_low, rope_high, rope_len0, row_positions, score_cap, score_slopes, score_spans) that are not 0."""
     return B.tn_llama_config(
         layers=cfg.layers, d_model=cfg.d_model, n_heads=cfg.n_heads, head_dim=cfg.head_dim, ffn=cfg.ffn,
         seq=cfg.seq, batch=cfg.batch, dtype=B.TN_F32 if cfg.dtype == "f32" else B.TN_BF16, tile=cfg.tile,
@@ -46,7 +51,7 @@ def llama_config_struct(cfg, kv_outputs: bool = False, weights_transposed: bool 
         hidden_outputs=int(hidden_outputs), output_layer_stride=int(output_layer_stride),
         decode_steps=int(getattr(cfg, "decode_steps", 0)), attn_whole_rows=int(attn_whole_rows),
         checkpoint_layers=int(checkpoint_layers), fuse_epilogues=int(fuse_epilogues),
-        recompute_normed=int(recompute_normed), recompute_gate_up=int(recompute_gate_up))
+        recompute_normed=int(recompute_normed), recompute_gate_up=int(recompute_gate_up), **(heads or {}))
 
 
 def bindings(tg) -> List[Tuple[int, str, int, int, int, int, int]]:
@@ -70,7 +75,7 @@ def export_taskgraph(tg) -> dict:
         params.append({f: getattr(x.params, f) for f, _ in B.tn_op_params._fields_})
         inputs.append(B.tn_taskgraph_inputs(tg, v) if x.n_inputs else [])
         shape.append((x.desc.rows, x.desc.cols))
-        dtype.append("f32" if x.desc.dtype == B.TN_F32 else "bf16")
+        dtype.append(_DTYPE_NAMES[x.desc.dtype])
         resid.append(x.residency)
         if x.output_index >= 0:
             outputs[x.output_index] = v
@@ -233,7 +238,7 @@ class GpuSession:
                  materialize_scores: bool = False, checkpoint: bool = False, device_outputs: bool = False,
                  device_inputs: bool = False, hidden_outputs: bool = False, output_layer_stride: int = 0,
                  attn_whole_rows: bool = False, checkpoint_layers: int = 0, fuse_epilogues: int = 0,
-                 recompute_normed: bool = False, recompute_gate_up: bool = False):
+                 recompute_normed: bool = False, recompute_gate_up: bool = False, heads: Optional[dict] = None):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("GpuSession needs a GPU; there is no CPU fallback")
@@ -243,7 +248,7 @@ class GpuSession:
                                                        lora_rank, train, k_split, materialize_scores,
                                                        checkpoint, hidden_outputs, output_layer_stride,
                                                        attn_whole_rows, checkpoint_layers, fuse_epilogues, recompute_normed,
-                                                       recompute_gate_up))
+                                                       recompute_gate_up, heads))
         self.cap = int(cap) if cap is not None else cap_for(cfg, self.tg)
         say = progress or (lambda msg: None)
         say("taskgraph built")
@@ -268,14 +273,14 @@ class GpuSession:
             if key not in seen:
                 seen[key] = total
                 cuts.append((total, a, r0, r1, c0, c1, tr))
-                total += ((r1 - r0) * (c1 - c0) * es + 255) // 256 * 256
+                total += ((r1 - r0) * (c1 - c0) * a.dtype.itemsize + 255) // 256 * 256
             offs[vid] = seen[key]
         self.in_slab = torch.empty(max(total, 256), dtype=torch.uint8).pin_memory()
         slab_np = self.in_slab.numpy()
         for off, a, r0, r1, c0, c1, tr in cuts:
             a = a.reshape(1, -1) if a.ndim == 1 else a
             tile = a[r0:r1, c0:c1]
-            dst = slab_np[off:off + tile.size * es].view(self.elem)
+            dst = slab_np[off:off + tile.size * a.dtype.itemsize].view(a.dtype)
             if tr:
                 np.copyto(dst.reshape(c1 - c0, r1 - r0), tile.T)
             else:

@@ -185,10 +185,13 @@ typedef struct {
  *                                       operands' type, zeros in a row that sees nothing
  *   ATTN_COMBINE finish                 1: as 0, but a row that no partial has seen a key of gives zeros; 2 -> fp32 [rows, hpg]: the log-sum-exp
  *                                       of the scores of rows [row0, row0 + rows), -inf for such a row (col0 == 0)
- *   ATTN_BWD     mode 4                 n_q_tiles, n_col_tiles, head_dim; operands: the finished attention O (tiles like Q), the
- *                                       dO tiles, one log-sum-exp (ATTN_COMBINE, finish 2) per Q row tile -> fp32 [q rows, 2*hpg]: what
- *                                       mode 0 gives, with D = sum O dO, and without forming the scores again.  With a score rule
- *                                       (trans_a == 0) modes 1 to 3 need no transposed grids.  The statistics of a rule come from mode 4. */
+ *   ATTN_BWD     mode 4                 n_q_tiles, n_col_tiles, head_dim, nk, row0; -> fp32 [q rows, 2*hpg]: what mode 0 gives, with
+ *                                       D = sum O dO and without forming the scores again.  nk == 0: operands the finished attention O
+ *                                       (tiles like Q), the dO tiles, one log-sum-exp (ATTN_COMBINE, finish 2) per Q row tile.  nk > 0: the
+ *                                       nk partials of the block, of whose rows the first is row0, then the dO tiles: O as it was before it
+ *                                       was rounded, which gradients of rows that see two or three keys need (bf16: O rounded puts
+ *                                       them up to 1e-2 off, this 2.5e-3).  With a score rule (trans_a == 0) modes 1 to 3 need no
+ *                                       transposed grids.  The statistics of a rule come from mode 4. */
 typedef struct {
   int32_t nk;
   int32_t d;

@@ -68,13 +68,13 @@ def attention(q, k, v, head_dim, scale, ok, cap=0.0, slopes=None, q_pos0=0, k_po
     return torch.cat(outs, 1), torch.stack(lses, 1)
 
 
-def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, slopes=None, q_pos0=0, k_pos0=0, do=None):
+def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, slopes=None, q_pos0=0, k_pos0=0, do=None, rounded_o=True):
     """How far correct results may lie from the exact ones, element by element: {"o", "lse"} and with `do` {"dq", "dk", "dv"}.
 
     Counted are the roundings a kernel makes: of stored results (`storage`: half a step relative to the value, 2^-8 or 2^-24), of weights
     and their gradients where they enter a product (`products`: 2^-8 for bf16 products, 0 for fp32), and those of fp32 arithmetic: of
     a score, one unit (2^-24) per term of its sum and a few more for scaling, cap, bias and the exponential; of a sum over n rows, n units;
-    O enters the reverse pass rounded to storage.  Below 2^-126, the smallest normal number, a weight, its gradient or a result may be zero."""
+    O enters the reverse pass rounded to storage, or (rounded_o False) as it was before.  Below 2^-126, the smallest normal number, a weight, its gradient or a result may be zero."""
     u, tiny = 2.0 ** -24, 2.0 ** -126
     out = {n: [] for n in ("o", "lse", "dq", "dk", "dv")}
     n = k.shape[0]
@@ -105,7 +105,8 @@ def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, s
         dt = 1 - t * t
         dp, D = dO @ V.T, (dO * o).sum(1, keepdim=True)
         e_dp = (head_dim + 8) * u * (dO.abs() @ V.abs().T)
-        e_D = (to * dO.abs()).sum(1, keepdim=True) + (head_dim + 8) * u * (o.abs() * dO.abs()).sum(1, keepdim=True)
+        to_D = to if rounded_o else (E + products + u * n) * A + tiny * (1 + V.abs().sum(0))
+        e_D = (to_D * dO.abs()).sum(1, keepdim=True) + (head_dim + 8) * u * (o.abs() * dO.abs()).sum(1, keepdim=True)
         ds = p * (dp - D) * dt * scale
         e_p = (E + 8 * u) * p + tiny
         e_ds = ds.abs() * (E + products + 16 * u) + p * scale * (dt * (e_dp + e_D) + (dp - D).abs() * (2 * t.abs() * (8 * u + raw * (head_dim + 8) * u / (cap or 1.0)) + 8 * u)) \

@@ -499,14 +499,17 @@ tn_status build_tables(tn_executor& ex) {
       case TN_OP_ATTN_BWD: {
         const int nq = x.p.n_q_tiles, nkv = x.p.n_kv_tiles, nc = x.p.n_col_tiles, hd = x.p.head_dim;
         if (x.p.mode == 4) {
+          const int first = x.p.nk > 0 ? x.p.nk : nq * nc;
           for (int c = 0; c < nc; ++c)
-            if (odesc(c).cols != odesc(0).cols) return fail(TN_ERR_SHAPE, "attn_bwd %lld: column tiles are not uniform", (long long)m);
+            if (odesc(first + c).cols != odesc(first).cols) return fail(TN_ERR_SHAPE, "attn_bwd %lld: column tiles are not uniform", (long long)m);
           for (int r = 0; r + 1 < nq; ++r)
-            if (odesc(r * nc).rows != odesc(0).rows || odesc((r + 1) * nc).rows > odesc(0).rows)
+            if (odesc(first + r * nc).rows != odesc(first).rows || odesc(first + (r + 1) * nc).rows > odesc(first).rows)
               return fail(TN_ERR_SHAPE, "attn_bwd %lld: Q row tiles are not uniform", (long long)m);
-          aux.insert(aux.end(), {odesc(0).rows, 0, odesc(0).cols, d.rows, 0});
+          aux.insert(aux.end(), {odesc(first).rows, 0, odesc(first).cols, d.rows, 0});
           vi.cls = LC_ATTN_STATS;
-          vi.bytes = 2.0 * d.rows * nc * odesc(0).cols * elem_bytes(d.dtype);
+          d.dtype = odesc(first).dtype;
+          vi.dtype = (int8_t)d.dtype;
+          vi.bytes = (double)d.rows * nc * odesc(first).cols * (elem_bytes(d.dtype) + (x.p.nk > 0 ? 4.0 * x.p.nk : elem_bytes(d.dtype)));
           break;
         }
         const int tq = odesc(0).rows, tk = odesc(nq * nc).rows, tc = odesc(0).cols;

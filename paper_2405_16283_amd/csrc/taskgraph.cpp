@@ -272,25 +272,30 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
       return TN_OK;
     case TN_OP_ATTN_BWD: {
       const int nq = p.n_q_tiles, nkv = p.n_kv_tiles, nc = p.n_col_tiles;
-      if (p.mode == 4) {  // statistics from O, dO and the log-sum-exp
-        if (nq < 1 || nc < 1 || p.head_dim < 1 || n_in != 2ll * nq * nc + nq)
-          return fail(TN_ERR_SHAPE, "attn_bwd: mode 4 needs 2 n_q_tiles * n_col_tiles operands and n_q_tiles log-sum-exps");
+      if (p.mode == 4) {  // statistics from O (or the partials it is joined from), dO and the log-sum-exp
+        const int first = p.nk > 0 ? p.nk : nq * nc;  // of the dO tiles
+        if (nq < 1 || nc < 1 || p.head_dim < 1 || p.nk < 0 || n_in != (p.nk > 0 ? p.nk + (int64_t)nq * nc : 2ll * nq * nc + nq))
+          return fail(TN_ERR_SHAPE, "attn_bwd: mode 4 needs the O tiles or nk partials, the dO tiles and, with O, n_q_tiles log-sum-exps");
         int64_t gw = 0, qrows = 0;
-        for (int c = 0; c < nc; ++c) gw += D(c).cols;
+        for (int c = 0; c < nc; ++c) gw += D(first + c).cols;
         if (gw % p.head_dim) return fail(TN_ERR_SHAPE, "attn_bwd: columns are not whole heads");
+        const int64_t hpg = gw / p.head_dim;
         for (int r = 0; r < nq; ++r) {
-          qrows += D(r * nc).rows;
+          qrows += D(first + r * nc).rows;
           for (int c = 0; c < nc; ++c) {
-            const auto& o = D(r * nc + c);
-            if (o.rows != D(r * nc).rows || o.cols != D(c).cols || o.dtype != D(0).dtype || !same(o, D((nq + r) * nc + c)))
+            const auto& o = D(first + r * nc + c);
+            if (o.rows != D(first + r * nc).rows || o.cols != D(first + c).cols || o.dtype != D(first).dtype || (p.nk == 0 && !same(o, D(r * nc + c))))
               return fail(TN_ERR_SHAPE, "attn_bwd: O / dO tile (%d,%d) does not fit the grid", r, c);
           }
+          if (p.nk > 0) continue;
           const auto& l = D(2 * nq * nc + r);
-          if (l.dtype != TN_F32 || l.rows != D(r * nc).rows || l.cols != gw / p.head_dim)
+          if (l.dtype != TN_F32 || l.rows != D(first + r * nc).rows || l.cols != hpg)
             return fail(TN_ERR_SHAPE, "attn_bwd: the log-sum-exp of Q row tile %d must be fp32 [rows, hpg]", r);
         }
-        if (out.dtype != TN_F32 || out.rows != qrows || out.cols != 2 * (gw / p.head_dim))
-          return fail(TN_ERR_SHAPE, "attn_bwd: output shape does not fit mode 4");
+        for (int k = 0; k < p.nk; ++k)
+          if (D(k).dtype != TN_F32 || D(k).cols != gw + 2 * hpg || D(k).rows != D(0).rows || p.row0 < 0 || p.row0 + qrows > D(0).rows)
+            return fail(TN_ERR_SHAPE, "attn_bwd: operand %d is not a partial of these rows", k);
+        if (out.dtype != TN_F32 || out.rows != qrows || out.cols != 2 * hpg) return fail(TN_ERR_SHAPE, "attn_bwd: output shape does not fit mode 4");
         return TN_OK;
       }
       if (has_rule(p) && (p.mode < 1 || p.trans_a))

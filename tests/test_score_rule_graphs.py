@@ -99,6 +99,13 @@ def test_score_rules(g):
                                ([do, do, lse], 10, 4, dict(head_dim=48)), ([do, do, lse], 10, 4, dict(n_q_tiles=2)), ([do, do, lse], 10, 4, dict(mode=5)),
                                ([do, do, spans], 10, 4, dict(spans=1))):
         _refused(g, R, ins, rows, cols, **{**dict(mode=4, n_q_tiles=1, n_col_tiles=1, head_dim=64), **p})
+    par = dict(mode=4, nk=2, n_q_tiles=1, n_col_tiles=1, head_dim=64)
+    assert g.op(R, [part, part, do], 10, 4, **par) >= 0
+    few = g.inp(4, 128)
+    assert g.op(R, [part, few], 4, 4, **{**par, "nk": 1, "row0": 6}) >= 0
+    for ins, rows, p in (([part, do], 10, {}), ([part, part, do, lse], 10, {}), ([do, do, do], 10, {}), ([part, g.inp(9, 132), do], 10, {}), ([part, part, do], 9, {}),
+                         ([part, part, do], 10, dict(row0=1)), ([part, part, do], 10, dict(row0=-1)), ([part, part, do], 10, dict(nk=-2)), ([part, few], 4, dict(nk=1, row0=7))):
+        _refused(g, R, ins, rows, 4, **{**par, **p})
     ins = [q, k, k, do, stats, slopes, spans]
     rule = dict(score_cap=5.0, slopes=1, spans=1)
     for mode, rows in ((1, 10), (2, 20), (3, 20)):

@@ -328,8 +328,7 @@ def _build(c, t):
     part = p.op(B.TN_OP_ATTN_BLOCK, flat(q) + flat(k) + flat(v) + slopes + spans, B.TN_F32, rows, d + 2 * heads, **par)
     r_, c_ = _cut(rows, c["tile"]), _cut(d, c["tile"])
     o = [[p.op(B.TN_OP_ATTN_COMBINE, [part], code, r1 - r0, c1 - c0, row0=r0, col0=c0, head_dim=hd, hpg=heads, finish=1) for c0, c1 in c_] for r0, r1 in r_]
-    lse = [p.op(B.TN_OP_ATTN_COMBINE, [part], B.TN_F32, r1 - r0, heads, row0=r0, head_dim=hd, hpg=heads, finish=2) for r0, r1 in r_]
-    stats = [p.op(B.TN_OP_ATTN_BWD, o[i] + do[i] + [lse[i]], B.TN_F32, r1 - r0, 2 * heads, mode=4, n_q_tiles=1, n_col_tiles=len(c_), head_dim=hd)
+    stats = [p.op(B.TN_OP_ATTN_BWD, [part] + do[i], B.TN_F32, r1 - r0, 2 * heads, mode=4, nk=1, row0=r0, n_q_tiles=1, n_col_tiles=len(c_), head_dim=hd)
              for i, (r0, r1) in enumerate(r_)]
     ins = flat(q) + flat(k) + flat(v) + flat(do) + stats + slopes + spans
     outs = {"o": flat(o)}

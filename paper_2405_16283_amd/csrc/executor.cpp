@@ -447,7 +447,7 @@ tn_status build_tables(tn_executor& ex) {
         break;
       }
       case TN_OP_ATTN_COMBINE:
-        vi.cls = x.p.finish == 2 ? LC_ATTN_LSE : x.p.finish ? LC_ATTN_JOIN : LC_ATTN_COMBINE;
+        vi.cls = x.p.finish == 2 ? LC_ATTN_LSE : !x.p.finish ? LC_ATTN_COMBINE : join_few(d) ? LC_ATTN_JOIN_FEW : LC_ATTN_JOIN;
         d.dtype = x.desc.dtype;
         vi.dtype = (int8_t)d.dtype;
         vi.bytes = x.bytes + d.n_in * ((double)d.rows * d.cols * 4.0);

@@ -96,6 +96,7 @@ enum LaunchClass {
   LC_ATTN_BWD_RULE_BF16_LAST = LC_ATTN_BWD_RULE_BF16 + 11,
   LC_ATTN_STATS,     // their statistics from O, dO and the log-sum-exp
   LC_ATTN_JOIN,      // combine with finish 1
+  LC_ATTN_JOIN_FEW,  // the same for few rows over many partials
   LC_ATTN_LSE,       // combine with finish 2
   LC_COUNT,
   // Not a class of its own for grouping: 128x128 tiles with two workgroups per CU, a form for launches of either of the two above.
@@ -209,6 +210,13 @@ hipError_t launch_gemm_rows(int dtype, const DeviceTables& t, uint32_t base, con
 // rule or finished rows have these behind them.
 enum { kRuleCap = 5, kRuleSlopes, kRuleSpans, kRuleFinish, kRuleAux };  // bits of score_cap; operand of the slopes and of the first spans, or -1
 
+// Which of the two a joining vertex of n_in partials goes to: where they are many and the rows few, a workgroup per row and head reads the
+// partials side by side instead of one after the other.  Launches, plain and so: 32 partials of 32 heads of 128, one row 11.1 and 6.2 us,
+// 64 rows 15.1 and 10.4, 128 rows 21.0 and 18.1; of 8 heads of 64, 128 rows 11.6 and 7.3.  8 partials: one row 6.0 and 6.0, 128 rows 6.8 and 12.0.
+inline bool join_few(const OpDesc& d) {
+  const int hd = d.p.head_dim;
+  return d.n_in >= 16 && (int64_t)d.rows * d.cols <= 512 * 1024 && hd % 4 == 0 && hd <= 1024 && d.p.hpg % 2 == 0 && d.p.col0 % hd == 0 && d.cols % hd == 0;
+}
 enum { kRuleHasCap = 1, kRuleHasSlopes = 2 };  // kernels of their own
 // LC_ATTN_RULE_BF16 to LC_ATTN_BWD_RULE_BF16_LAST: attn_rule.hip.
 inline bool is_attn_rule_bf16(int cls) { return cls >= LC_ATTN_RULE_BF16 && cls <= LC_ATTN_BWD_RULE_BF16_LAST; }

@@ -432,6 +432,55 @@ __global__ void __launch_bounds__(256) attn_combine_kernel(DeviceTables t, Batch
   st((T*)d.out + (size_t)row * d.cols + c, num / den);
 }
 
+// Few rows over many partials (a token's attention, split over a long cache): a workgroup to a row and head.  Its threads take a partial
+// each for the weights, then four columns of every G-th partial; both sums are finished in a fixed order by way of LDS.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_join_few_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  __shared__ float weight[256], waves[8];
+  __shared__ f32x4 part[256];
+  const int hd = d.p.head_dim, hpg = d.p.hpg, gw = hd * hpg, ldp = gw + 2 * hpg, heads = d.cols / hd;
+  const int row = blockIdx.x / heads, h = d.p.col0 / hd + blockIdx.x % heads, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const size_t r = (size_t)(d.p.row0 + row) * ldp;
+  auto partial = [&](int j) { return (const float*)t.ptrs[d.ptr0 + j] + r; };
+  float m = -INFINITY;
+  for (int j = tid; j < d.n_in; j += 256) m = fmaxf(m, get_global(partial(j) + gw + h));
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if (lane == 0) waves[w] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+  if (m == -INFINITY) m = 0.f;
+  const int per = hd / 4, groups = max(1, 256 / per), c = tid % per * 4, g = tid / per;
+  float den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = 0; j0 < d.n_in; j0 += 256) {
+    const int n = min(256, d.n_in - j0);
+    __syncthreads();
+    if (tid < n) {
+      const float* p = partial(j0 + tid);
+      const float e = __expf(get_global(p + gw + h) - m);
+      weight[tid] = e;
+      den = fmaf(get_global(p + gw + hpg + h), e, den);
+    }
+    __syncthreads();
+    if (g < groups) {
+#pragma unroll 4
+      for (int j = g; j < n; j += groups) num += get_global((const f32x4*)(partial(j0 + j) + h * hd + c)) * weight[j];
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) den += __shfl_xor(den, off, 64);
+  if (lane == 0) waves[4 + w] = den;
+  part[tid] = num;
+  __syncthreads();
+  if (g > 0) return;
+  den = (waves[4] + waves[5]) + (waves[6] + waves[7]);
+  for (int k = 1; k < groups; ++k) num += part[k * per + tid];
+  st4((T*)d.out + (size_t)row * d.cols + (h * hd - d.p.col0) + c, den == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : num / den);
+}
+
 // The log-sum-exp of a row and head over the partials of its block, -inf where none has seen a key.
 __global__ void __launch_bounds__(256) attn_lse_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
@@ -1354,6 +1403,7 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
     case LC_HEAD_GAIN_EIGHTS:
     case LC_COL_SUM: return head_blocks(cls, d, aux);
     case LC_ATTN_STATS: return cdiv((int64_t)d.rows * (d.p.n_col_tiles * aux[d.aux0 + 2] / d.p.head_dim), 16);
+    case LC_ATTN_JOIN_FEW: return d.rows * (d.cols / d.p.head_dim);
     case LC_ATTN_LSE: return cdiv((int64_t)d.rows * d.cols, 256);
     case LC_ATTN_RULE_F32:
     case LC_ATTN_F32: {
@@ -1459,6 +1509,7 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
       if (bf) hipLaunchKernelGGL((attn_combine_kernel<bf16_t, true>), grid, wg, 0, s, t, b);
       else hipLaunchKernelGGL((attn_combine_kernel<float, true>), grid, wg, 0, s, t, b);
       break;
+    case LC_ATTN_JOIN_FEW: TN_LAUNCH_T(attn_join_few_kernel); break;
     case LC_ATTN_LSE: hipLaunchKernelGGL(attn_lse_kernel, grid, wg, 0, s, t, b); break;
     case LC_ATTN_STATS: TN_LAUNCH_T(attn_stats_kernel); break;
     case LC_SILU_MUL:

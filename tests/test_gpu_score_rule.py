@@ -266,6 +266,41 @@ def test_padding_behind_the_last_sequence(dtype):
         assert (a[139:] == 0).all(), n
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,heads,hd,parts,col0,cols", [(1, 4, 64, 16, 0, 256), (1, 4, 64, 15, 0, 256), (1, 2, 128, 300, 0, 256), (3, 6, 64, 33, 128, 192), (5, 2, 128, 19, 128, 128),
+                                                            (2, 2, 1024, 17, 0, 2048), (3, 4, 20, 70, 20, 40), (1, 3, 64, 20, 0, 192), (2, 2, 64, 12, 32, 64)])
+def test_joins_of_few_rows(rows, heads, hd, parts, col0, cols, dtype):
+    """Partials as any attention leaves them, some of a row that saw nothing, one row that no partial has seen a key of."""
+    rng = np.random.default_rng(9)
+    d = heads * hd
+    P = rng.standard_normal((parts, rows, d + 2 * heads)).astype(np.float32)
+    P[..., d:d + heads] *= 20
+    P[..., d + heads:] = np.abs(P[..., d + heads:]) + 1
+    empty = rng.random((parts, rows)) < 0.3
+    empty[:, -1] |= rows > 1
+    P[empty] = 0
+    P[empty, d:d + heads] = -np.inf
+    g = Graph(dtype)
+    ins = [g.inp(p, "f32") for p in P]
+    out, lse = g.run([g.op(B.TN_OP_ATTN_COMBINE, ins, rows, cols, col0=col0, head_dim=hd, hpg=heads, finish=1),
+                      g.op(B.TN_OP_ATTN_COMBINE, ins, rows, heads, "f32", head_dim=hd, hpg=heads, finish=2)])
+    P = P.astype(np.float64)
+    m, l = P[..., d:d + heads], P[..., d + heads:]
+    top = np.where(np.isinf(m.max(0)), 0, m.max(0))
+    w = np.exp(m - top)
+    den = (w * l).sum(0)
+    num = (P[..., :d].reshape(parts, rows, heads, hd) * w[..., None]).sum(0)
+    size = (np.abs(P[..., :d]).reshape(parts, rows, heads, hd) * w[..., None]).sum(0)
+    safe = np.where(den == 0, 1, den)[..., None]
+    ref, size = (a.reshape(rows, d)[:, col0:col0 + cols] for a in (num / safe, size / safe))
+    # weights: exponents of up to 80 in 24 bits, 80 units; sums over the partials, a unit each; one rounding to storage
+    tol = (parts + 200) * 2.0 ** -24 * size + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref)
+    assert (np.abs(out - ref) <= tol).all()
+    with np.errstate(divide="ignore"):
+        want = top + np.log(den)
+    _within(lse, want, (parts + 200) * 2.0 ** -24 * (1 + np.abs(np.where(np.isinf(want), 0, want))), "lse")
+
+
 @pytest.mark.parametrize("rows,keys,causal", [(2, 2, 1), (3, 3, 1), (40, 2, 0), (64, 3, 0)])
 def test_gradients_of_rows_that_see_few_keys(rows, keys, causal):
     """bf16, statistics from partials: the gradients as a whole are off by no more than the two roundings they cannot do without (of dS, and of the

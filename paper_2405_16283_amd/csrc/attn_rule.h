@@ -77,5 +77,83 @@ struct Rule {
   }
 };
 
+// minimum over the wavefront, as a scalar: exchanges inside the vector unit for each sixteen lanes, the four by scalars
+template <int CTRL>
+__device__ __forceinline__ int exchanged(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false); }
+__device__ __forceinline__ int wave_min(int v) {
+  v = min(v, exchanged<0xB1>(v));   // neighbours
+  v = min(v, exchanged<0x4E>(v));   // pairs
+  v = min(v, exchanged<0x141>(v));  // the mirrored half of eight
+  v = min(v, exchanged<0x140>(v));  // of sixteen
+  return min(min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+
+// Head and row block of a workgroup: the blocks that see most go first, of all heads, so that none of them is started when the others
+// are nearly done.  Two workgroups share a compute unit from the start, the n-th and the one a chipful later: the first chipful goes
+// from its smallest to its largest, so that the largest share theirs with the smallest of the second.  Where the heads
+// are a multiple of 8, every XCD gets heads of its own, whose keys and values its L2 then serves to all their row blocks.
+constexpr int kComputeUnits = 256;
+__device__ __forceinline__ void head_and_rank(int bx, int total, int hpg, int& h, int& rank) {
+  if ((hpg & 7) == 0) {
+    const int per = hpg >> 3, one_each = min(kComputeUnits, total) >> 3;
+    int n = bx >> 3;
+    if (n < one_each) n = one_each - 1 - n;
+    h = (bx & 7) * per + n % per;
+    rank = n / per;
+  } else {
+    if (bx < kComputeUnits) bx = min(kComputeUnits, total) - 1 - bx;
+    h = bx % hpg;
+    rank = bx / hpg;
+  }
+}
+
+// Whose turn is `rank`-th of `blocks` blocks of ROWS rows (queries, or keys)?  Without spans late queries and early keys see most under a
+// causal mask.  With spans it goes by what a block's first and last row see: an estimate, which decides the order and nothing
+// else.  Every workgroup finds the same order, each thread the place of one block (of at most 256; beyond, the order without spans).
+// Three packed documents in 4096 rows of 32 heads: forward 123 us in the order without spans, 98 so, dQ 151 and 117, dK 247 and 178, dV 208 and
+// 156.  (All heads' largest blocks before any smaller one costs nothing over one head after the other where launches are long.)
+template <int ROWS, bool OWN_Q>
+__device__ __forceinline__ int block_of_rank(const Rule& rule, int rank, int blocks, int my_rows, int q_rows, int* shared) {
+  const int plain = OWN_Q ? blocks - 1 - rank : rank;
+  if (!rule.spans || blocks > 256) return plain;
+  const int tid = threadIdx.x;
+  int mine = -1;
+  if (tid < blocks) {
+    mine = 0;
+    int first = INT_MAX, behind = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = e ? min(my_rows, (tid + 1) * ROWS) - 1 : tid * ROWS;
+      if (OWN_Q) {
+        int lo, hi;
+        rule.visible(row, lo, hi);
+        if (lo < hi) {
+          first = min(first, lo);
+          behind = max(behind, hi);
+        }
+      } else {  // queries from the one at the key's own position to the end of that one's span
+        const int q = min(max(row + rule.k_pos0 - rule.q_pos0, 0), q_rows - 1);
+        first = min(first, q);
+        behind = max(behind, rule.span_end(q, q_rows));
+      }
+    }
+    if (first < behind) mine = behind - first;
+  }
+  shared[tid] = mine;
+  __syncthreads();
+  int place = 0;
+  for (int j = 0; j < blocks; j += 4) {
+    const int4 v = *(const int4*)(shared + j);
+    const int e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) place += e[k] > mine || (e[k] == mine && j + k < tid);
+  }
+  if (tid < blocks && place == rank) shared[256] = tid;
+  __syncthreads();
+  const int block = __builtin_amdgcn_readfirstlane(shared[256]);
+  __syncthreads();
+  return block;
+}
+
 }  // namespace
 }  // namespace tn

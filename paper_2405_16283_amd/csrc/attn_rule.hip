@@ -40,17 +40,6 @@ __device__ __forceinline__ int swizzle(int row) {
   return HD == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 2) << 1) | ((row >> 2) & 3);
 }
 
-// minimum over the wavefront, as a scalar: exchanges inside the vector unit for each sixteen lanes, the four by scalars
-template <int CTRL>
-__device__ __forceinline__ int exchanged(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false); }
-__device__ __forceinline__ int wave_min(int v) {
-  v = min(v, exchanged<0xB1>(v));   // neighbours
-  v = min(v, exchanged<0x4E>(v));   // pairs
-  v = min(v, exchanged<0x141>(v));  // the mirrored half of eight
-  v = min(v, exchanged<0x140>(v));  // of sixteen
-  return min(min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
-}
-
 // A lane's own row as MFMA operand: 16-byte pieces 2 s + g of head h.  One tile: its address is the wavefront's.
 template <int HD>
 __device__ __forceinline__ void load_own(void* const* tiles, int n_tiles, int nc, int trows, int tc, int row, int h, int g, bf16x8 (&v)[HD / 16]) {
@@ -60,68 +49,6 @@ __device__ __forceinline__ void load_own(void* const* tiles, int n_tiles, int nc
   else p = tile_elem<bf16_t>(tiles, nc, trows, tc, row, h * HD);
 #pragma unroll
   for (int s = 0; s < HD / 16; ++s) v[s] = get_global((const bf16x8*)(p + s * 16 + g * 8));
-}
-
-// Head and row block of a workgroup: the blocks that see most go first, of all heads, so that none of them is started when the others
-// are nearly done.  Where the heads are a multiple of 8, every XCD gets heads of its own, whose keys and values its L2 then serves to
-// all their row blocks.
-__device__ __forceinline__ void head_and_rank(int bx, int hpg, int& h, int& rank) {
-  if ((hpg & 7) == 0) {
-    const int per = hpg >> 3, n = bx >> 3;
-    h = (bx & 7) * per + n % per;
-    rank = n / per;
-  } else {
-    h = bx % hpg;
-    rank = bx / hpg;
-  }
-}
-
-// Whose turn is `rank`-th of `blocks` blocks of kRuleRows rows (queries, or keys)?  Without spans late queries and early keys see most under a
-// causal mask.  With spans it goes by what a block's first and last row see: an estimate, which decides the order and nothing
-// else.  Every workgroup finds the same order, each thread the place of one block (of at most 256; beyond, the order without spans).
-// Three packed documents in 4096 rows of 32 heads: forward 123 us in the order without spans, 98 so, dQ 151 and 117, dK 247 and 178, dV 208 and
-// 156.  (All heads' largest blocks before any smaller one costs nothing over one head after the other where launches are long.)
-template <bool OWN_Q>
-__device__ __forceinline__ int block_of_rank(const Rule& rule, int rank, int blocks, int my_rows, int q_rows, int* shared) {
-  const int plain = OWN_Q ? blocks - 1 - rank : rank;
-  if (!rule.spans || blocks > 256) return plain;
-  const int tid = threadIdx.x;
-  int mine = -1;
-  if (tid < blocks) {
-    mine = 0;
-    int first = INT_MAX, behind = 0;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int row = e ? min(my_rows, (tid + 1) * kRuleRows) - 1 : tid * kRuleRows;
-      if (OWN_Q) {
-        int lo, hi;
-        rule.visible(row, lo, hi);
-        if (lo < hi) {
-          first = min(first, lo);
-          behind = max(behind, hi);
-        }
-      } else {  // queries from the one at the key's own position to the end of that one's span
-        const int q = min(max(row + rule.k_pos0 - rule.q_pos0, 0), q_rows - 1);
-        first = min(first, q);
-        behind = max(behind, rule.span_end(q, q_rows));
-      }
-    }
-    if (first < behind) mine = behind - first;
-  }
-  shared[tid] = mine;
-  __syncthreads();
-  int place = 0;
-  for (int j = 0; j < blocks; j += 4) {
-    const int4 v = *(const int4*)(shared + j);
-    const int e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) place += e[k] > mine || (e[k] == mine && j + k < tid);
-  }
-  if (tid < blocks && place == rank) shared[256] = tid;
-  __syncthreads();
-  const int block = __builtin_amdgcn_readfirstlane(shared[256]);
-  __syncthreads();
-  return block;
 }
 
 template <int HD, bool CAP, bool SLOPES>
@@ -137,8 +64,8 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
   const int nc = d.p.n_col_tiles, gw = nc * tc, hpg = gw / HD;
   const Rule rule(t, d);
   int h, rb;
-  head_and_rank(blockIdx.x, hpg, h, rb);
-  rb = block_of_rank<true>(rule, rb, (q_rows + kRuleRows - 1) / kRuleRows, q_rows, q_rows, (int*)lds);
+  head_and_rank(blockIdx.x, d.nblocks, hpg, h, rb);
+  rb = block_of_rank<kRuleRows, true>(rule, rb, (q_rows + kRuleRows - 1) / kRuleRows, q_rows, q_rows, (int*)lds);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, g = lane >> 5;
   void* const* Qp = t.ptrs + d.ptr0;
   void* const* Kp = Qp + d.p.n_q_tiles * nc;
@@ -382,8 +309,8 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
   const int my_rows = OWN_Q ? q_rows : kv_rows, o_rows = OWN_Q ? kv_rows : q_rows, my_trows = OWN_Q ? tq : tk, o_trows = OWN_Q ? tk : tq;
   const Rule rule(t, d);
   int h, rb;
-  head_and_rank(blockIdx.x, hpg, h, rb);
-  rb = block_of_rank<OWN_Q>(rule, rb, (my_rows + kRuleRows - 1) / kRuleRows, my_rows, q_rows, (int*)lds);
+  head_and_rank(blockIdx.x, d.nblocks, hpg, h, rb);
+  rb = block_of_rank<kRuleRows, OWN_Q>(rule, rb, (my_rows + kRuleRows - 1) / kRuleRows, my_rows, q_rows, (int*)lds);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, g = lane >> 5;
   const int row0 = rb * kRuleRows + w * 32, row = row0 + l32;
   const bool exists = row < my_rows;

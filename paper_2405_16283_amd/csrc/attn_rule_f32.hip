@@ -1,0 +1,269 @@
+// Attention by a score rule with fp32 products (MFMA 16x16x4), for tile grids whose heads and chunks of keys lie inside one tile; others
+// go to attn_f32.hip.
+//
+// One workgroup = one head x 32 query rows.  Two wavefronts own 16 of them each, twice: the second pair takes every second chunk of
+// keys, and the two states are joined at the end.  As there, scores are formed transposed, S^T = K Q^T, which leaves a lane (n =
+// lane & 15, g = lane >> 4) the weights of its own query n against keys 4 g + i of 16: the B operand of O^T += V^T P^T if step c of four
+// products takes keys 4 g + c.
+//
+// Keys and values come 8 KiB of each at a time (32 keys of heads of 64, 16 of heads of 128) by direct global-to-LDS loads into two stages,
+// one chunk ahead.  The 16-byte pieces of a row are stored in an order that depends on the row, so that neither the reads of K (one
+// piece of 16 rows) nor those of V (16 columns of rows 4 g + c) meet in a bank.
+//
+// Bound: the matrix cores (a chunk costs a wavefront 64 products of 32 cycles) and, in small launches, the longest of the walks over the keys: 32
+// rows instead of 64 put two workgroups on a compute unit, a long one and a short one.  1024 positions of 16 heads of 64, causal, with
+// slopes: 70 us with 64 rows and chunks by way of registers, 43 so, 37 in the order of head_and_rank (the products alone would take
+// 14); 64 such heads 268 -> 124 us, 8 heads of 128 125 -> 59.  Where every row sees every key the matrix cores are busy half the time (77
+// TFLOP/s): two wavefronts share one, and both wait at the barrier of every chunk.
+#include "attn_rows.h"
+
+#include <climits>
+#include <type_traits>
+
+namespace tn {
+namespace {
+
+constexpr int kOwnRows = 32;           // query rows of a workgroup
+constexpr int kOperand = 8192;         // bytes of a chunk of K or V
+typedef __attribute__((address_space(3))) const f32x4* lds_f32x4;
+typedef __attribute__((address_space(3))) const float* lds_f32;
+
+template <int HD>
+__global__ void __launch_bounds__(256, 2) attn_rule_f32_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  constexpr int KEYS = kOperand / (4 * HD), CPR = HD / 4, KT = KEYS / 16, NLD = kOperand / 2048;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int* ax = t.aux + d.aux0;
+  const int tq = ax[0], tk = ax[1], tc = ax[2], q_rows = ax[3], kv_rows = ax[4];
+  const int nc = d.p.n_col_tiles, gw = nc * tc, hpg = gw / HD;
+  const Rule rule(t, d);
+  int h, rb;
+  head_and_rank(blockIdx.x, d.nblocks, hpg, h, rb);
+  rb = block_of_rank<kOwnRows, true>(rule, rb, (q_rows + kOwnRows - 1) / kOwnRows, q_rows, q_rows, (int*)lds);
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 1, part = wave >> 1;
+  void* const* Qp = t.ptrs + d.ptr0;
+  void* const* Kp = Qp + d.p.n_q_tiles * nc;
+  void* const* Vp = Kp + d.p.n_kv_tiles * nc;
+  const Side<float, HD> Q(Qp, nc, tq, tc, q_rows, h);
+  const int row = rb * kOwnRows + w * 16 + n;
+  const bool exists = row < q_rows;
+  f32x4 q[HD / 16];
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) q[j] = Q.at(min(row, q_rows - 1), 16 * j + 4 * g);
+  int lo = 0, hi = 0;
+  if (exists) rule.visible(row, lo, hi);
+  const float slope = rule.slope(h);
+  // of the wavefront: what some row sees, and what all rows that exist see
+  const int w_begin = wave_min(lo < hi ? lo : INT_MAX), w_end = -wave_min(-hi);
+  const int all_lo = -wave_min(exists ? -lo : INT_MAX), all_hi = wave_min(exists ? hi : INT_MAX);
+  int begin, end;  // of the workgroup
+  {
+    int* const shared = (int*)lds;
+    if (lane == 0) {
+      shared[2 * wave] = w_begin;
+      shared[2 * wave + 1] = w_end;
+    }
+    __syncthreads();
+    begin = min(shared[0], shared[2]);
+    end = max(shared[1], shared[3]);
+    begin = begin < end ? begin & ~(KEYS - 1) : end;
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    end = __builtin_amdgcn_readfirstlane(end);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) q[j] *= d.p.scale;
+  f32x4 o[HD / 16];
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) o[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  // LDS: of either part two stages of K, then V.  Piece p = i * 128 + thread of a chunk is stored at byte 16 p: row r = p / CPR, of K there
+  // piece (p % CPR) ^ (r & 15), of V piece (p % CPR) ^ (r & 12).
+  const uint32_t mine = (uint32_t)(size_t)(lptr_t)lds + part * 4 * kOperand;
+  const int ct = (h * HD) / tc, cin0 = (h * HD) % tc;
+  auto issue = [&](int kv0, int stage) {
+    const int rt = kv0 / tk, kin = kv0 - rt * tk, trows = min(tk, kv_rows - rt * tk);
+    const float* Kt = (const float*)sload_ptr((const void* const*)(Kp + rt * nc + ct));
+    const float* Vt = (const float*)sload_ptr((const void* const*)(Vp + rt * nc + ct));
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(mine + stage * 2 * kOperand + w * 1024);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) {
+      const int p = i * 128 + (threadIdx.x & 127), r = p / CPR, c = p % CPR;
+      const size_t at = (size_t)min(kin + r, trows - 1) * tc + cin0;  // rows past the end: one that exists, hidden below
+      load_lds(Kt + at + (c ^ (r & 15)) * 4, dst + i * 2048);
+      load_lds(Vt + at + (c ^ (r & 12)) * 4, dst + kOperand + i * 2048);
+    }
+  };
+  uint32_t k_at[HD / 16], v_at[HD / 16];  // in the first stage
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) {
+    k_at[j] = mine + n * (HD * 4) + ((4 * j + g) ^ n) * 16;
+    v_at[j] = mine + kOperand + 4 * g * (HD * 4) + ((4 * j + (n >> 2)) ^ (4 * g)) * 16 + (n & 3) * 4;
+  }
+  auto chunk = [&](int kv0, auto stage) {
+    constexpr int at = decltype(stage)::value * 2 * kOperand;
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this chunk has arrived
+    __syncthreads();                     // ... for everybody, and everybody is done with the other stage
+    if (kv0 + 2 * KEYS < end) issue(kv0 + 2 * KEYS, 1 - decltype(stage)::value);
+    if (kv0 + KEYS <= w_begin || kv0 >= w_end) return;
+    f32x4 s[KT], s2[KT];  // even and odd steps of the head apart: chains of products enough
+#pragma unroll
+    for (int k = 0; k < KT; ++k) s[k] = s2[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < HD / 16; j += 2) {
+      f32x4 a[KT], a2[KT];
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        a[k] = *(lds_f32x4)(size_t)(k_at[j] + (at + k * 16 * (HD * 4)));
+        a2[k] = *(lds_f32x4)(size_t)(k_at[j + 1] + (at + k * 16 * (HD * 4)));
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          s[k] = mfma_f32(a[k][c], q[j][c], s[k]);
+          s2[k] = mfma_f32(a2[k][c], q[j + 1][c], s2[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < KT; ++k) s[k] += s2[k];
+    // element i of s[k]: key kv0 + 16 k + 4 g + i
+    if (rule.cap > 0.f) {
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[k][i] = rule.cap * tanh_f32(s[k][i] * rule.inv_cap);
+    }
+    if (rule.slopes) {
+      const float base = (float)(rule.q_pos0 + row - rule.k_pos0 - kv0 - 4 * g);
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[k][i] = fmaf(-slope, fabsf(base - (float)(16 * k + i)), s[k][i]);
+    }
+    if (kv0 < all_lo || kv0 + KEYS > all_hi) {
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int kv = kv0 + 16 * k + 4 * g + i;
+          if (kv < lo || kv >= hi) s[k][i] = -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[k][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mn = fmaxf(m, mx), ms = mn == -INFINITY ? 0.f : mn;  // nothing visible yet: every weight is exp(-inf)
+    if (__any(mn > m)) {
+      const float alpha = __expf(m - ms);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) o[j] *= alpha;
+    }
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[k][i] = __expf(s[k][i] - ms);
+        l += s[k][i];
+      }
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) o[j] = mfma_f32(*(lds_f32)(size_t)(v_at[j] + (at + (16 * k + c) * (HD * 4))), s[k][c], o[j]);
+  };
+  const int from = begin + part * KEYS;
+  if (from < end) issue(from, 0);
+  // (both parts pass as many barriers: the second may have no last chunk)
+  for (int kv0 = from; kv0 - part * KEYS < end; kv0 += 4 * KEYS) {
+    chunk(kv0, std::integral_constant<int, 0>{});
+    if (kv0 - part * KEYS + 2 * KEYS < end) chunk(kv0 + 2 * KEYS, std::integral_constant<int, 1>{});
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  // the second part's state by way of LDS
+  {
+    f32x4* const theirs = (f32x4*)lds;
+    float* const stats = (float*)(lds + 2 * 64 * (HD / 16) * 16);
+    __syncthreads();
+    if (part) {
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) theirs[(w * (HD / 16) + j) * 64 + lane] = o[j];
+      stats[w * 64 + lane] = m;
+      stats[128 + w * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (part) return;
+    const float m2 = stats[w * 64 + lane], l2 = stats[128 + w * 64 + lane];
+    const float mn = fmaxf(m, m2), ms = mn == -INFINITY ? 0.f : mn, w1 = __expf(m - ms), w2 = __expf(m2 - ms);
+    m = mn;
+    l = l * w1 + l2 * w2;
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) o[j] = o[j] * w1 + theirs[(w * (HD / 16) + j) * 64 + lane] * w2;
+  }
+  // a weight of zero times an infinity or NaN of a key the row does not see: such rows are formed again
+  float z = 0.f;
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z = fmaf(o[j][i], 0.f, z);
+  if (__builtin_expect(__any(exists && !(z == 0.f)), 0)) {
+    const int first = rb * kOwnRows + w * 16;
+    return attn_by_rows<float, HD, true>(t, d, h, first, first + 16, lane >> 4, 4);
+  }
+  if (!exists) return;
+  if (ax[kRuleFinish]) {
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) st4_finished((float*)d.out + (size_t)row * gw + h * HD + 16 * j + 4 * g, o[j], l);
+    return;
+  }
+  float* out = (float*)d.out + (size_t)row * d.cols;
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) {
+    float* o4 = out + h * HD + 16 * j + 4 * g;
+    if ((d.cols & 3) == 0) {  // rows of the partial are 16-byte aligned
+      st4(o4, o[j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o4[i] = o[j][i];
+    }
+  }
+  if (g == 0) {
+    out[gw + h] = m;
+    out[gw + hpg + h] = l;
+  }
+}
+
+template <int HD>
+hipError_t launch(const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
+  constexpr int lds = 8 * kOperand;
+  if (const hipError_t e = allow_lds(allowed, (const void*)attn_rule_f32_kernel<HD>, lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(attn_rule_f32_kernel<HD>, dim3((unsigned)max_blocks, (unsigned)b.n), dim3(256), lds, s, t, b);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int32_t attn_rule_f32_blocks(const OpDesc& d, const int32_t* aux) {
+  const int32_t* ax = aux + d.aux0;
+  return d.p.n_col_tiles * ax[2] / d.p.head_dim * ((ax[3] + kOwnRows - 1) / kOwnRows);
+}
+
+hipError_t launch_attn_rule_f32(int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+  if (head_dim == 64) return launch<64>(t, b, max_blocks, s);
+  if (head_dim == 128) return launch<128>(t, b, max_blocks, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace tn

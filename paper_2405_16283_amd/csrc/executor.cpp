@@ -431,6 +431,8 @@ tn_status build_tables(tn_executor& ex) {
           // the bf16 kernel wants plain V tiles, whole heads inside one column tile and 64-key chunks inside one row tile
           vi.cls = (d.dtype == TN_BF16 && !x.p.v_trans && tc % hd == 0 && (nkv == 1 || tk % 64 == 0))
                        ? (int8_t)(LC_ATTN_RULE_BF16 + rule_kernel(x.p)) : (int8_t)LC_ATTN_RULE_F32;
+          // so does the fp32 kernel for whole tiles, of chunks of 2048 / head_dim keys
+          if (d.dtype == TN_F32 && !x.p.v_trans && tc % hd == 0 && (nkv == 1 || tk % (2048 / hd) == 0)) vi.cls = LC_ATTN_RULE_F32_TILES;
           vi.head_dim = (int16_t)hd;
           vi.flops = 4.0 * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
           vi.bytes = (q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
@@ -701,6 +703,7 @@ int family_of(int cls) {
     case LC_ATTN_BWD_BF16_DK:
     case LC_ATTN_BWD_BF16_DV:
     case LC_ATTN_RULE_F32:
+    case LC_ATTN_RULE_F32_TILES:
     case LC_ATTN_BWD_RULE: return 1;
     default: return is_attn_rule_bf16(cls) ? 1 : 2;
   }

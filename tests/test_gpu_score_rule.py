@@ -66,12 +66,17 @@ CASES = {
                           spans=_window(70, 50, first=2 ** 30 - 70)),
     "heads across tiles": dict(rows=100, keys=100, heads=2, hd=128, tile=64, cap=8.0, slopes=1),
     "transposed": dict(rows=140, keys=140, heads=2, hd=64, v_trans=1, cap=8.0, spans=_documents(140, [50])),
+    "odd tiles": dict(rows=130, keys=171, heads=3, hd=64, row_tile=50, q_pos0=41, cap=8.0, slopes=1, spans=_window(130, 90, first=41)),
+    "tiles of sixteen": dict(rows=60, keys=75, heads=2, hd=128, row_tile=16, causal=0, cap=8.0, spans=_holes(60, 75, 4)),
+    "more blocks than compute units": dict(rows=1100, keys=1100, heads=8, hd=64, spans=_documents(1100, [300, 310, 900])),
+    "more of odd heads": dict(rows=1000, keys=300, heads=9, hd=64, causal=0, slopes=1, k_pos0=100),
+    "blocks without an order": dict(rows=8300, keys=40, heads=1, hd=64, causal=0, cap=6.0, spans=_holes(8300, 40, 3)),
 }
 
 
 class Case:
     def __init__(self, c, dtype, seed=0):
-        self.c = c = {**dict(tile=0, causal=1, cap=0.0, slopes=0, spans=None, q_pos0=0, k_pos0=0, v_trans=0, std=2.0), **c}
+        self.c = c = {**dict(tile=0, row_tile=0, causal=1, cap=0.0, slopes=0, spans=None, q_pos0=0, k_pos0=0, v_trans=0, std=2.0), **c}
         rng = np.random.default_rng(seed)
         d = c["heads"] * c["hd"]
         self.dtype, self.d = dtype, d
@@ -92,7 +97,7 @@ class Case:
     def add(self, g):
         """Input vertices (Q, K, V, dO tiles, slopes, spans) and the tiles' shape."""
         c = self.c
-        rt, ct = c["tile"] or max(c["rows"], c["keys"]), c["tile"] or self.d
+        rt, ct = c["row_tile"] or c["tile"] or max(c["rows"], c["keys"]), c["tile"] or self.d
         self.rt, self.ct = rt, ct
         self.nq, self.nkv, self.nc = -(-c["rows"] // rt), -(-c["keys"] // rt), -(-self.d // ct)
         self.Q, self.K, self.dO = (g.grid(a, rt, ct) for a in (self.q, self.k, self.do))

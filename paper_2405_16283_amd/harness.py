@@ -15,6 +15,7 @@ _TENSOR_NAMES = {B.TN_T_X: "x", B.TN_T_WQ: "wq", B.TN_T_WK: "wk", B.TN_T_WV: "wv
                  B.TN_T_BV: "bv", B.TN_T_PROBE: "probe", B.TN_T_DAQ: "daq", B.TN_T_DBQ: "dbq", B.TN_T_DAV: "dav",
                  B.TN_T_DBV: "dbv", B.TN_T_DX: "dx", B.TN_T_H: "h", B.TN_T_GQ: "gq", B.TN_T_GK: "gk", B.TN_T_POS: "positions",
                  B.TN_T_SPANS: "spans", B.TN_T_SLOPES: "slopes"}
+_ELEMENTS = {"positions": np.int32, "spans": np.int32, "slopes": np.float32}  # of the other tensors: the configuration's
 OUTPUT_TENSORS = ("y", "k", "v", "daq", "dbq", "dav", "dbv", "dx", "h")
 OP_NAMES = {B.TN_OP_INPUT: "input", B.TN_OP_GEMM: "gemm", B.TN_OP_RMS_STAT: "rms_stat",
             B.TN_OP_RMS_APPLY: "rms_apply", B.TN_OP_ROPE: "rope", B.TN_OP_ATTN_BLOCK: "attn_block",
@@ -23,6 +24,8 @@ OP_NAMES = {B.TN_OP_INPUT: "input", B.TN_OP_GEMM: "gemm", B.TN_OP_RMS_STAT: "rms
             B.TN_OP_RMS_BWD_APPLY: "rms_bwd_apply", B.TN_OP_ATTN_BWD: "attn_bwd", B.TN_OP_TRANSPOSE: "transpose",
             B.TN_OP_SUM: "sum", B.TN_OP_SOFTMAX_STAT: "softmax_stat", B.TN_OP_SOFTMAX_APPLY: "softmax_apply",
             B.TN_OP_HEAD_ROPE: "head_rope", B.TN_OP_HEAD_ROPE_BWD: "head_rope_bwd", B.TN_OP_COL_SUM: "col_sum"}
+_HEAD_FIELDS = ("qk_norm", "rope_half", "rotary_dim", "rope_factor", "rope_low", "rope_high", "rope_len0", "row_positions",
+                "score_cap", "score_slopes", "score_spans")
 _DTYPE_NAMES = {B.TN_F32: "f32", B.TN_BF16: "bf16", B.TN_I32: "i32"}
 MG_KIND_NAMES = {B.TN_MG_INPUT: "input", B.TN_MG_LOAD: "load", B.TN_MG_OP: "op", B.TN_MG_OFFLOAD: "offload",
                  B.TN_MG_RELOAD: "reload", B.TN_MG_DROP: "drop", B.TN_MG_STORE: "store", B.TN_MG_JOIN: "join"}
@@ -39,6 +42,8 @@ def llama_config_struct(cfg, kv_outputs: bool = False, weights_transposed: bool 
                         heads: Optional[dict] = None) -> B.tn_llama_config:
     """workloads.LlamaConfig -> tn_llama_config.  heads: the fields of tn_llama_config on heads and scores (qk_norm, rope_half,
     rotary_dim, rope_factor, rope_low, rope_high, rope_len0, row_positions, score_cap, score_slopes, score_spans) that are not 0."""
+    if unknown := set(heads or {}) - set(_HEAD_FIELDS):
+        raise ValueError(f"heads: no such fields: {sorted(unknown)}")
     return B.tn_llama_config(
         layers=cfg.layers, d_model=cfg.d_model, n_heads=cfg.n_heads, head_dim=cfg.head_dim, ffn=cfg.ffn,
         seq=cfg.seq, batch=cfg.batch, dtype=B.TN_F32 if cfg.dtype == "f32" else B.TN_BF16, tile=cfg.tile,
@@ -272,15 +277,16 @@ class GpuSession:
             key = (id(a), r0, r1, c0, c1, tr)
             if key not in seen:
                 seen[key] = total
-                cuts.append((total, a, r0, r1, c0, c1, tr))
-                total += ((r1 - r0) * (c1 - c0) * a.dtype.itemsize + 255) // 256 * 256
+                elem = np.dtype(_ELEMENTS.get(name, self.elem))
+                cuts.append((total, a, elem, r0, r1, c0, c1, tr))
+                total += ((r1 - r0) * (c1 - c0) * elem.itemsize + 255) // 256 * 256
             offs[vid] = seen[key]
         self.in_slab = torch.empty(max(total, 256), dtype=torch.uint8).pin_memory()
         slab_np = self.in_slab.numpy()
-        for off, a, r0, r1, c0, c1, tr in cuts:
+        for off, a, elem, r0, r1, c0, c1, tr in cuts:
             a = a.reshape(1, -1) if a.ndim == 1 else a
             tile = a[r0:r1, c0:c1]
-            dst = slab_np[off:off + tile.size * a.dtype.itemsize].view(a.dtype)
+            dst = slab_np[off:off + tile.size * elem.itemsize].view(elem)
             if tr:
                 np.copyto(dst.reshape(c1 - c0, r1 - r0), tile.T)
             else:

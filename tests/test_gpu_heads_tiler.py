@@ -21,12 +21,16 @@ def _orders_agree(s, out):
             np.testing.assert_array_equal(again[k], out[k])
 
 
-@pytest.mark.parametrize("options", C.OPTIONS)
-@pytest.mark.parametrize("name,kw", [("ragged_f32", {}), ("batch2_f32", dict(v_transposed=False, attn_whole_rows=True)), ("decode_f32", dict(v_transposed=False))])
+def _runs(*forms):
+    """Every form with all options that it takes (spans instead of the causal mask do not go with decode steps)."""
+    return [pytest.param(n, kw, o, id=f"{n}-{i}-{o}") for i, (n, kw) in enumerate(forms) for o in C.OPTIONS
+            if not (n.startswith("decode") and C.OPTIONS[o].get("score_spans") == 2)]
+
+
+@pytest.mark.parametrize("name,kw,options", _runs(("ragged_f32", {}), ("batch2_f32", dict(v_transposed=False, attn_whole_rows=True)),
+                                                  ("decode_f32", dict(v_transposed=False))))
 def test_prefill_and_decode_fp32(name, kw, options):
     cfg, full, wide, heads = C.case(name, options)
-    if cfg.decode_steps and heads.get("score_spans") == 2:
-        pytest.skip("refused")
     s = H.GpuSession(cfg, full, heads=heads, **kw)
     try:
         out, rep = s.run(OPTS)
@@ -36,14 +40,11 @@ def test_prefill_and_decode_fp32(name, kw, options):
         s.close()
 
 
-@pytest.mark.parametrize("options", C.OPTIONS)
-@pytest.mark.parametrize("name,kw", [("ragged_bf16", dict(v_transposed=False)), ("ragged_bf16", dict(v_transposed=True)),
-                                     ("decode_bf16", dict(v_transposed=False, fuse_epilogues=3))])
+@pytest.mark.parametrize("name,kw,options", _runs(("ragged_bf16", dict(v_transposed=False)), ("ragged_bf16", dict(v_transposed=True)),
+                                                  ("decode_bf16", dict(v_transposed=False, fuse_epilogues=3))))
 def test_prefill_and_decode_bf16(name, kw, options):
     cfg, full, wide, heads = C.case(name, options)
     cfg = cfg.with_(layers=1)  # as the other bf16 graphs: two layers of two correct pipelines drift apart
-    if cfg.decode_steps and heads.get("score_spans") == 2:
-        pytest.skip("refused")
     s = H.GpuSession(cfg, full, heads=heads, **kw)
     try:
         out, rep = s.run(OPTS)
@@ -94,3 +95,20 @@ def test_inputs_already_in_place_are_not_copied_again():
         np.testing.assert_array_equal(s.outputs()["y"], first["y"])
     finally:
         s.close()
+
+
+def test_arrays_of_other_types_are_converted_or_refused():
+    """As before tensors of integers were inputs: what converts without a change of kind does, and nothing is taken for its bytes."""
+    cfg, full, wide, heads = C.case("batch2_f32", "everything")
+    other = {k: a.astype(np.int64 if a.dtype == np.int32 else np.float64) for k, a in full.items()}
+    got = []
+    for inputs in (full, other):
+        s = H.GpuSession(cfg, inputs, heads=heads)
+        try:
+            got.append(s.run(OPTS)[0]["y"])
+        finally:
+            s.close()
+    np.testing.assert_array_equal(*got)
+    cfg, full, wide, heads = C.case("ragged_bf16", "plain")
+    with pytest.raises(TypeError):
+        H.GpuSession(cfg, {**full, "x": wide["x"].astype(np.float32)})

@@ -875,7 +875,7 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
   // what the reverse pass needs of the forward pass, per layer and sequence, indexed by row tile
   struct Saved {
     Grid xin, a, q, k, v, h1, gate, up;
-    Grid qpre, kpre, o, lse;  // with qk_norm: the rotation's operands; with a score rule: finished attention and log-sum-exps
+    Grid qpre, kpre, part;  // with qk_norm: the rotation's operands; with a score rule: the partials of the stripe that the tile is of
     std::vector<tn_vid> rstd1, rstd2, tq, tv;
   };
   std::vector<std::vector<Saved>> saved(c.train ? c.layers : 0, std::vector<Saved>(c.batch));
@@ -906,7 +906,7 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
     if (sv) {
       sv->xin = xb;
       for (Grid* gp : {&sv->a, &sv->q, &sv->k, &sv->v, &sv->h1, &sv->gate, &sv->up}) gp->assign(t.rows.size(), {});
-      for (Grid* gp : {&sv->qpre, &sv->kpre, &sv->o, &sv->lse}) gp->assign(t.rows.size(), {});
+      for (Grid* gp : {&sv->qpre, &sv->kpre, &sv->part}) gp->assign(t.rows.size(), {});
       for (auto* vp : {&sv->rstd1, &sv->rstd2, &sv->tq, &sv->tv}) vp->assign(t.rows.size(), -1);
     }
     Grid kk(t.rows.size()), vv(t.rows.size());  // K, V of the stripes done so far
@@ -1004,10 +1004,13 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
         // key block (its online softmax runs over the whole range; one partial instead of s + 1)
         // (score_spans 2: over all keys there are)
         const size_t last = two_sided ? stripes.size() - 1 : s;
+        // Training by a rule does so as well: its reverse pass takes the statistics from that one partial, fp32, where rows that see
+        // two or three keys would not bear finished rows in bf16.
+        const bool whole = c.attn_whole_rows || (c.train && rule);
         // with a rule a vertex that sees all keys of one row tile leaves finished rows, and no combine is needed
         const bool finished = rule && c.attn_whole_rows && rt.size() == 1 && ctg == 1;
-        for (size_t s2 = c.attn_whole_rows ? last : 0; s2 <= last; ++s2) {
-          const int32_t k_from = c.attn_whole_rows ? 0 : stripes[s2].a;
+        for (size_t s2 = whole ? last : 0; s2 <= last; ++s2) {
+          const int32_t k_from = whole ? 0 : stripes[s2].a;
           std::vector<size_t> kt;
           for (size_t i = 0; i < t.rows.size(); ++i)
             if (t.rows[i].a >= k_from && t.rows[i].a < stripes[s2].b) kt.push_back(i);
@@ -1045,15 +1048,7 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
                                       {c.dtype, t.rows[i].len(), t.dcols[gi * ctg + cc].len()});
           }
         if (sv && rule)  // (train: a head group is one column tile)
-          for (size_t i : rt) {
-            tn_op_params p{};
-            p.finish = 2;
-            p.row0 = t.rows[i].a - stripes[s].a;
-            p.head_dim = c.head_dim;
-            p.hpg = hpg;
-            sv->lse[i].push_back(t.op(TN_OP_ATTN_COMBINE, p, parts, {TN_F32, t.rows[i].len(), hpg}));
-            sv->o[i].push_back(o[i][gi]);
-          }
+          for (size_t i : rt) sv->part[i].push_back(parts[0]);
       }
       // output projection, residual, feed-forward, residual -- row tile by row tile
       for (size_t i : rt) {
@@ -1346,7 +1341,9 @@ tn_status tn_build_llama(const tn_llama_config* cfg, tn_taskgraph** out) {
             ps.mode = 4;
             ps.n_q_tiles = ps.n_col_tiles = 1;
             ps.head_dim = c.head_dim;
-            stats[i] = t.op(TN_OP_ATTN_BWD, ps, {sv.o[i][j], dO[i][j], sv.lse[i][j]}, {TN_F32, m, 2 * hpg_});
+            ps.nk = 1;
+            ps.row0 = t.rows[i].a % c.attn_block;
+            stats[i] = t.op(TN_OP_ATTN_BWD, ps, {sv.part[i][j], dO[i][j]}, {TN_F32, m, 2 * hpg_});
             std::vector<tn_vid> in{sv.q[i][j]};
             for (size_t r = 0; r < to; ++r) in.push_back(sv.k[r][j]);
             for (size_t r = 0; r < to; ++r) in.push_back(vn[r]);

@@ -101,3 +101,26 @@ def test_refusals():
     for h in (dict(score_cap=1.0), dict(score_slopes=1), dict(score_spans=1)):
         refused(cfg, h, materialize_scores=True)
     refused(C.config("decode_f32"), dict(score_spans=2))
+
+
+def test_unknown_fields_of_heads_are_refused():
+    for wrong in ("scor_cap", "layers", "tile"):
+        with pytest.raises(ValueError, match=wrong):
+            H.llama_config_struct(C.config("c1"), heads={"score_cap": 1.0, wrong: 1})
+
+
+@pytest.mark.parametrize("kw", [{}, dict(checkpoint=True)])
+def test_training_by_a_rule_takes_its_statistics_from_one_partial(kw):
+    """Of finished rows in bf16 they put gradients of rows that see two or three keys up to 1e-2 off."""
+    cfg, full, wide, heads = C.case("batch2_f32", "documents", lora=True)
+    tg = B.tn_build_llama(H.llama_config_struct(cfg, heads=heads, lora_rank=16, train=True, **kw))
+    try:
+        x = H.export_taskgraph(tg)
+        stats = [v for v, k in enumerate(x["kind"]) if k == "attn_bwd" and x["params"][v]["mode"] == 4]
+        assert stats
+        for v in stats:
+            ins = x["inputs"][v]
+            assert x["params"][v]["nk"] == 1 and len(ins) == 2 and x["kind"][ins[0]] == "attn_block" and x["dtype"][ins[0]] == "f32"
+            assert x["params"][ins[0]]["k_pos0"] == 0
+    finally:
+        B.tn_taskgraph_destroy(tg)

@@ -9,6 +9,8 @@
 #include "device.h"
 #include "kernels.h"
 
+#include <algorithm>
+
 namespace tn {
 namespace {
 
@@ -69,51 +71,52 @@ struct Head {
 };
 
 constexpr int kPer = 8;  // pairs per lane: heads of up to 1024 elements
+constexpr int64_t kGenericBlocks = 1 << 18;  // far more wavefronts than the chip holds, and far from what a launch may have
 
-// Any head size: a wavefront per row and head, lane by lane through its pairs.
+// Any head size: a wavefront per row and head at a time, lane by lane through its pairs.
 template <typename T>
 __global__ void __launch_bounds__(256) head_rope_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
   const Head s(t, d);
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (int64_t)s.rows * s.heads) return;
-  const int row = (int)(id / s.heads), h = (int)(id % s.heads);
-  const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
-  const T* x = (const T*)t.ptrs[d.ptr0] + at;
-  const T* gain = s.norm ? (const T*)t.ptrs[d.ptr0 + 1] : nullptr;
-  T* o = (T*)d.out + at;
-  float va[kPer], vb[kPer], ss = 0.f;
+  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * 4) {
+    const int row = (int)(id / s.heads), h = (int)(id % s.heads);
+    const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
+    const T* x = (const T*)t.ptrs[d.ptr0] + at;
+    const T* gain = s.norm ? (const T*)t.ptrs[d.ptr0 + 1] : nullptr;
+    T* o = (T*)d.out + at;
+    float va[kPer], vb[kPer], ss = 0.f;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = lane + 64 * k;
-    va[k] = vb[k] = 0.f;
-    if (i >= s.head_dim / 2) continue;
-    int ea, eb;
-    s.pairs.elements(i, ea, eb);
-    va[k] = ld(x + ea);
-    vb[k] = ld(x + eb);
-    ss += va[k] * va[k] + vb[k] * vb[k];
-  }
-  const float r = s.norm ? s.rstd(wave_sum(ss)) : 1.f;
-  const double pos = s.position(row);
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = lane + 64 * k;
-    if (i >= s.head_dim / 2) continue;
-    int ea, eb;
-    s.pairs.elements(i, ea, eb);
-    float a = va[k], c = vb[k];
-    if (s.norm) {
-      a *= r * ld(gain + ea);
-      c *= r * ld(gain + eb);
+    for (int k = 0; k < kPer; ++k) {
+      const int i = lane + 64 * k;
+      va[k] = vb[k] = 0.f;
+      if (i >= s.head_dim / 2) continue;
+      int ea, eb;
+      s.pairs.elements(i, ea, eb);
+      va[k] = ld(x + ea);
+      vb[k] = ld(x + eb);
+      ss += va[k] * va[k] + vb[k] * vb[k];
     }
-    float sn = 0.f, cs = 1.f;
-    if (s.pairs.turns(i)) turn(pos, s.turns[i], sn, cs);
-    if (d.p.mode) sn = -sn;
-    st(o + ea, a * cs - c * sn);
-    st(o + eb, a * sn + c * cs);
+    const float r = s.norm ? s.rstd(wave_sum(ss)) : 1.f;
+    const double pos = s.position(row);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int i = lane + 64 * k;
+      if (i >= s.head_dim / 2) continue;
+      int ea, eb;
+      s.pairs.elements(i, ea, eb);
+      float a = va[k], c = vb[k];
+      if (s.norm) {
+        a *= r * ld(gain + ea);
+        c *= r * ld(gain + eb);
+      }
+      float sn = 0.f, cs = 1.f;
+      if (s.pairs.turns(i)) turn(pos, s.turns[i], sn, cs);
+      if (d.p.mode) sn = -sn;
+      st(o + ea, a * cs - c * sn);
+      st(o + eb, a * sn + c * cs);
+    }
   }
 }
 
@@ -147,33 +150,33 @@ __global__ void __launch_bounds__(256) head_rope_bwd_kernel(DeviceTables t, Batc
   if ((int)blockIdx.x >= d.nblocks) return;
   const Head s(t, d);
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (int64_t)s.rows * s.heads) return;
-  const int row = (int)(id / s.heads), h = (int)(id % s.heads);
-  const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
-  const T* gain = (const T*)t.ptrs[d.ptr0 + 2];
-  float ua[kPer], ub[kPer], xa[kPer], xb[kPer], dot = 0.f;
-  const float r = load_reverse(s, (const T*)t.ptrs[d.ptr0] + at, (const T*)t.ptrs[d.ptr0 + 1] + at, s.position(row), lane, ua, ub, xa, xb);
-  T* o = (T*)d.out + at;
+  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * 4) {
+    const int row = (int)(id / s.heads), h = (int)(id % s.heads);
+    const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
+    const T* gain = (const T*)t.ptrs[d.ptr0 + 2];
+    float ua[kPer], ub[kPer], xa[kPer], xb[kPer], dot = 0.f;
+    const float r = load_reverse(s, (const T*)t.ptrs[d.ptr0] + at, (const T*)t.ptrs[d.ptr0 + 1] + at, s.position(row), lane, ua, ub, xa, xb);
+    T* o = (T*)d.out + at;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = lane + 64 * k;
-    if (i >= s.head_dim / 2) continue;
-    int ea, eb;
-    s.pairs.elements(i, ea, eb);
-    ua[k] *= ld(gain + ea);
-    ub[k] *= ld(gain + eb);
-    dot += ua[k] * xa[k] + ub[k] * xb[k];
-  }
-  const float m = wave_sum(dot) * r * r / (float)s.head_dim;  // mean(u gain n) * rsqrt(..): the second rsqrt(..) is n's below
+    for (int k = 0; k < kPer; ++k) {
+      const int i = lane + 64 * k;
+      if (i >= s.head_dim / 2) continue;
+      int ea, eb;
+      s.pairs.elements(i, ea, eb);
+      ua[k] *= ld(gain + ea);
+      ub[k] *= ld(gain + eb);
+      dot += ua[k] * xa[k] + ub[k] * xb[k];
+    }
+    const float m = wave_sum(dot) * r * r / (float)s.head_dim;  // mean(u gain n) * rsqrt(..): the second rsqrt(..) is n's below
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = lane + 64 * k;
-    if (i >= s.head_dim / 2) continue;
-    int ea, eb;
-    s.pairs.elements(i, ea, eb);
-    st(o + ea, r * (ua[k] - xa[k] * m));
-    st(o + eb, r * (ub[k] - xb[k] * m));
+    for (int k = 0; k < kPer; ++k) {
+      const int i = lane + 64 * k;
+      if (i >= s.head_dim / 2) continue;
+      int ea, eb;
+      s.pairs.elements(i, ea, eb);
+      st(o + ea, r * (ua[k] - xa[k] * m));
+      st(o + eb, r * (ub[k] - xb[k] * m));
+    }
   }
 }
 
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(256) head_gain_kernel(DeviceTables t, Batch b)
   const Head s(t, d);
   __shared__ float part[4][1024];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int row0 = blockIdx.x * kGainRows, n = min(kGainRows, s.rows - row0);
+  const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
   float ga[kPer], gb[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) ga[k] = gb[k] = 0.f;
@@ -211,14 +214,16 @@ __global__ void __launch_bounds__(256) head_gain_kernel(DeviceTables t, Batch b)
     part[w][eb] = gb[k];
   }
   __syncthreads();
-  float* o = (float*)d.out + (size_t)blockIdx.x * s.head_dim;
+  float* o = (float*)d.out + (size_t)block * s.head_dim;
   for (int c = threadIdx.x; c < s.head_dim; c += 256) o[c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
 }
 
 // ---- heads of a multiple of 16 elements, pairs that come in eights ---------------------------------
 // Eight pairs to a lane -- two runs of eight elements, 16-byte accesses -- and a head to 4, 8, 16 .. lanes, of which those past its end
 // are idle.  What bounds these is memory; a lane's angles, 8 of them with 64-bit products, are formed once for the heads it walks
-// over, as many as leave enough wavefronts to fill the chip (kHeadWalk).
+// over, as many as leave enough wavefronts to fill the chip (kHeadWalk).  16384 rows of 32 heads of 128, bf16, with norm: 53 us (268 MB,
+// 5.1 TB/s), the gradient 72 (403 MB, 5.6 TB/s); by wavefronts of a pair to a lane (the kernels above) 218 and 340.  One row: 6.6 us, a
+// launch and three dependent loads.
 
 // eight elements as loaded, which may be on their way while the head before them is worked on
 template <typename T>
@@ -437,16 +442,20 @@ __global__ void __launch_bounds__(256) head_rope_bwd_eights_kernel(DeviceTables 
 }
 
 // Sums of the gain's gradient: the lanes of a head keep to one row at a time and walk over its heads; what the groups of a wavefront
-// and the wavefronts of the workgroup have summed is added in a fixed order.
+// and the wavefronts of the workgroup have summed is added in a fixed order.  Blocks of rows go from the last to the first: the gradient
+// of the input, formed from the same operands, leaves its last ones in the caches.  16384 rows of 32 heads of 128, bf16: 55 us (268
+// MB, 4.9 TB/s), from the first row on 63.  64 rows: 18 us, sixteen heads one behind the other; with 256 threads, which take 32,
+// 23; with 1024 17, but three heads of 64 in fp32 14 instead of 9, since registers spill.
+constexpr int kGainThreads = 512;
 template <typename T>
-__global__ void __launch_bounds__(256) head_gain_eights_kernel(DeviceTables t, Batch b) {
+__global__ void __launch_bounds__(kGainThreads) head_gain_eights_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
   const Head s(t, d);
   const Eights e(s);
-  __shared__ float part[4][1024];
-  const int row0 = blockIdx.x * kGainRows, n = min(kGainRows, s.rows - row0);
-  const int groups = 256 / e.lanes, group = threadIdx.x / e.lanes;
+  __shared__ float part[kGainThreads / 64][1024];
+  const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
+  const int groups = kGainThreads / e.lanes, group = threadIdx.x / e.lanes;
   const int per_row = max(1, groups / kGainRows);  // groups that share a row
   float ga[8] = {}, gb[8] = {};
   for (int r = group / per_row; r < n; r += groups / per_row) {
@@ -501,12 +510,17 @@ __global__ void __launch_bounds__(256) head_gain_eights_kernel(DeviceTables t, B
     }
   }
   __syncthreads();
-  float* o = (float*)d.out + (size_t)blockIdx.x * s.head_dim;
-  for (int c = threadIdx.x; c < s.head_dim; c += 256) o[c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+  float* o = (float*)d.out + (size_t)block * s.head_dim;
+  for (int c = threadIdx.x; c < s.head_dim; c += kGainThreads) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kGainThreads / 64; ++w) sum += part[w][c];
+    o[c] = sum;
+  }
 }
 
 // Sum of all rows of the operands: a workgroup per 32 columns, eight threads to a column, each every eighth row; their sums are
-// added in order.
+// added in order.  (512 rows of 128 columns 5 us: 64 loads one behind the other in four workgroups.)
 __global__ void __launch_bounds__(256) col_sum_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
@@ -537,7 +551,7 @@ int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   const int64_t heads = cls == LC_COL_SUM ? 0 : ax[kHeadCols] / d.p.head_dim;
   switch (cls) {
     case LC_HEAD_ROPE:
-    case LC_HEAD_ROPE_BWD: return (int32_t)((ax[kHeadRows] * heads + 3) / 4);
+    case LC_HEAD_ROPE_BWD: return (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + 3) / 4, kGenericBlocks);
     case LC_HEAD_ROPE_EIGHTS:
     case LC_HEAD_ROPE_BWD_EIGHTS:
       return (int32_t)((ax[kHeadRows] * ((heads + ax[kHeadWalk] - 1) / ax[kHeadWalk]) * head_lanes(d.p.head_dim) + 255) / 256);
@@ -561,7 +575,10 @@ hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& 
     case LC_HEAD_GAIN: TN_LAUNCH(head_gain_kernel); break;
     case LC_HEAD_ROPE_EIGHTS: TN_LAUNCH(head_rope_eights_kernel); break;
     case LC_HEAD_ROPE_BWD_EIGHTS: TN_LAUNCH(head_rope_bwd_eights_kernel); break;
-    case LC_HEAD_GAIN_EIGHTS: TN_LAUNCH(head_gain_eights_kernel); break;
+    case LC_HEAD_GAIN_EIGHTS:
+      if (bf) hipLaunchKernelGGL(head_gain_eights_kernel<bf16_t>, grid, dim3(kGainThreads), 0, s, t, b);
+      else hipLaunchKernelGGL(head_gain_eights_kernel<float>, grid, dim3(kGainThreads), 0, s, t, b);
+      break;
     case LC_COL_SUM: hipLaunchKernelGGL(col_sum_kernel, grid, wg, 0, s, t, b); break;
     default: return hipErrorInvalidValue;
   }

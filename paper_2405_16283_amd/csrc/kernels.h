@@ -229,8 +229,9 @@ enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadR
 constexpr int kGainRows = 32;  // rows to a sum of the gain's gradient
 // Heads of a multiple of 16 elements whose pairs come in eights go to the kernels for those: 16 elements to a lane, a head to a power of
 // two of lanes.  A lane's angles serve all the heads of its row that it walks over; it walks over fewer where there are few
-// rows, down to one, so that the chip has wavefronts enough.
-constexpr int64_t kHeadLanes = 1 << 18;
+// rows, down to one, so that the chip has wavefronts enough.  Launches of 32 heads of 128, walking over 1, 2, 4 and 8 heads: 512 rows 8.4,
+// 8.3, 9.4 and 11.8 us; 1024 11.4, 9.8, 10.2, 12.4; 2048 18.2, 14.1, 12.4, 14.0; 4096 31.3, 23.7, 20.3, 18.1.
+constexpr int64_t kHeadLanes = 1 << 17;
 inline bool head_by_eights(const int32_t* ax, int32_t head_dim) { return head_dim % 16 == 0 && (!ax[kHeadHalf] || ax[kHeadRotary] % 16 == 0); }
 __host__ __device__ inline int head_lanes(int head_dim) {
   int n = 1;

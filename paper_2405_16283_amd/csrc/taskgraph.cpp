@@ -203,6 +203,8 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
           return fail(TN_ERR_SHAPE, "attn_combine: finish 2 gives fp32 [rows, hpg] of rows inside the block");
         return TN_OK;
       }
+      if (p.finish == 1 && (int64_t)out.rows * out.cols / (out.cols % 4 || p.col0 % 4 || p.head_dim % 4 ? 1 : 4) >= INT32_MAX)
+        return fail(TN_ERR_SHAPE, "attn_combine: a window of finished rows of 2^31 elements and more (2^33 if whole fours)");  // counted in 32 bits
       if (p.row0 < 0 || p.col0 < 0 || p.row0 + out.rows > D(0).rows || p.col0 + out.cols > gw)
         return fail(TN_ERR_SHAPE, "attn_combine: output window leaves the block");
       return TN_OK;
@@ -280,6 +282,7 @@ tn_status validate_op(const TaskGraph& g, int32_t kind, const tn_op_params& p, c
         for (int c = 0; c < nc; ++c) gw += D(first + c).cols;
         if (gw % p.head_dim) return fail(TN_ERR_SHAPE, "attn_bwd: columns are not whole heads");
         const int64_t hpg = gw / p.head_dim;
+        if (hpg * out.rows >= 1 << 28) return fail(TN_ERR_SHAPE, "attn_bwd: mode 4 takes fewer than 2^28 rows times heads");  // sixteen threads to each
         for (int r = 0; r < nq; ++r) {
           qrows += D(first + r * nc).rows;
           for (int c = 0; c < nc; ++c) {

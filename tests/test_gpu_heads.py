@@ -172,3 +172,9 @@ def test_sums_of_columns():
         (out,) = g.run([g.op(B.TN_OP_COL_SUM, [g.inp(p) for p in parts], 1, cols, "f32")])
         a = np.concatenate(parts).astype(np.float64)
         assert (np.abs(out[0] - a.sum(0)) <= len(a) * U * np.abs(a).sum(0)).all()
+
+
+def test_more_heads_than_a_launch_has_wavefronts():
+    c = dict(rows=300001, heads=4, hd=6)
+    test_forward(c, "f32")
+    test_backward(c, "f32")

@@ -134,3 +134,14 @@ def test_integer_inputs_take_four_bytes_each(g):
     assert [B.tn_memgraph_vertex(mg, v).bytes for v in range(3)] == [2560, 40, 2560]
     B.tn_memgraph_simulate(mg)
     B.tn_memgraph_destroy(mg)
+
+
+def test_sizes_past_what_a_launch_counts(g):
+    C, R = B.TN_OP_ATTN_COMBINE, B.TN_OP_ATTN_BWD
+    rows = 2 ** 25
+    part, odd = g.inp(rows, 2 * 64 + 4), g.inp(2 ** 26, 2 * 33 + 4)
+    assert g.op(C, [part], rows, 128, head_dim=64, hpg=2, finish=1) >= 0
+    _refused(g, C, [odd], 2 ** 26, 66, head_dim=33, hpg=2, finish=1)
+    assert g.op(C, [odd], 2 ** 24, 66, head_dim=33, hpg=2, finish=1) >= 0
+    do = g.inp(2 ** 27, 2)
+    _refused(g, R, [do, do, do], 2 ** 27, 4, mode=4, n_q_tiles=1, n_col_tiles=1, head_dim=1)

@@ -332,3 +332,38 @@ def test_every_order_and_the_static_tables_give_the_same_bits(dtype):
     first = once(1)
     for again in (once(2), once(3), once(4, True)):
         assert all((a == b).all() for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_cache_of_more_than_4_gib(dtype):
+    """Heads rotated in a tensor of 4.1 GiB and attended to at its beginning and behind 4 GiB; one vertex is values and source of keys."""
+    d, hd, n = 4096, 128, 40
+    keys = ((1 << 32) + (1 << 27)) // (d * (4 if dtype == "f32" else 2))
+    rng = np.random.default_rng(9)
+    g = Graph(dtype)
+    cache = torch.zeros((keys, d), dtype=torch.float32 if dtype == "f32" else torch.bfloat16)
+    first, last = rounded(rng.standard_normal((n, d)), dtype), rounded(rng.standard_normal((n, d)), dtype)
+    cache[:n], cache[-n:] = torch.from_numpy(first), torch.from_numpy(last)
+    kv = B.tn_taskgraph_add_input(g.tg, B.TN_F32 if dtype == "f32" else B.TN_BF16, keys, d, B.TN_HOST)
+    g.host[kv] = cache if dtype == "f32" else cache.view(torch.int16)
+    q, do = rounded(rng.standard_normal((2, d)), dtype), rounded(rng.standard_normal((2, d)), dtype)
+    spans = np.array([[3, n], [keys - n, keys]])
+    scale = float(np.float32(hd ** -0.5))
+    Q, dO, S = g.inp(q), g.inp(do), g.inp(spans, "i32")
+    K = g.op(B.TN_OP_HEAD_ROPE, [kv], keys, d, head_dim=hd, rope_base=1e4, rope_half=1)
+    rule = dict(n_q_tiles=1, n_kv_tiles=1, n_col_tiles=1, head_dim=hd, scale=scale, spans=1, score_cap=20.0)
+    out = g.op(B.TN_OP_ATTN_BLOCK, [Q, K, kv, S], 2, d, finish=1, **rule)
+    part = g.op(B.TN_OP_ATTN_BLOCK, [Q, K, kv, S], 2, d + 64, "f32", **rule)
+    stats = g.op(B.TN_OP_ATTN_BWD, [part, dO], 2, 64, "f32", mode=4, nk=1, n_q_tiles=1, n_col_tiles=1, head_dim=hd)
+    dq = g.op(B.TN_OP_ATTN_BWD, [Q, K, kv, dO, stats, S], 2, d, mode=1, **rule)
+    got, grad = g.run([out, dq], cap=3 * (1 << 32) + (1 << 28) + (1 << 27))
+    freq = H.frequencies(hd, 1e4, 0.0, 0, 1.0, 4.0)
+    for row, (rows, lo) in enumerate(((first[3:], 3), (last, keys - n))):
+        k = H.head_rotate(torch.tensor(rows), hd, torch.arange(lo, lo + len(rows)), freq, True)
+        k = torch.tensor(rounded(k.numpy(), dtype))
+        x = torch.tensor(q[row:row + 1], requires_grad=True)
+        o, _ = H.attention(x, k, torch.tensor(rows), hd, scale, torch.ones(1, len(rows), dtype=torch.bool), 20.0, None, 0, 0)
+        (gq,) = torch.autograd.grad(o, x, torch.tensor(do[row:row + 1]))
+        # a wrong row anywhere is an error of the order of 1; the rotated keys' rounding may differ by a step where the sine does
+        for a, b in ((got[row], o.detach().numpy()[0]), (grad[row], gq.numpy()[0])):
+            assert np.linalg.norm(a - b) <= (1e-5 if dtype == "f32" else 2e-2) * np.linalg.norm(b)

@@ -1,4 +1,4 @@
-// Attention by a score rule with fp32 products (MFMA 16x16x4), for tile grids whose heads and chunks of keys lie inside one tile; others
+// Attention by a score rule with fp32 products (MFMA 16x16x4), forward and reverse, for tile grids whose heads and chunks of keys lie inside one tile; others
 // go to attn_f32.hip.
 //
 // One workgroup = one head x 32 query rows.  Two wavefronts own 16 of them each, twice: the second pair takes every second chunk of
@@ -244,26 +244,282 @@ __global__ void __launch_bounds__(256, 2) attn_rule_f32_kernel(DeviceTables t, B
   }
 }
 
+// Reverse pass, in the same way: modes 1 (dQ; own rows are queries, keys and values come in chunks), 2 (dK) and 3 (dV; own rows are
+// keys, queries and dO come in chunks, with what the queries' statistics say and what they see).  Scores are formed again, p = exp(score - lse),
+// and acc^T[column, own row] += X^T[column, other row] w[other row, own row] with X = K, Q or dO: of the chunk of K (Q) both a piece of 16 rows
+// and 16 columns of rows 4 g + c are read, so pieces are stored at (piece ^ (row & 15)), which suits either.
+// All three gradients, one launch, against the kernels of attn_f32.hip (64 own rows, chunks by way of registers): 320 packed rows of 3 heads of 64 31 -> 19
+// us, 1024 causal rows with slopes of 16 heads of 64 217 -> 131, of 64 heads 732 -> 446, 8 heads of 128 with a cap 207 -> 163.
+constexpr int kStatBytes = 512;  // of a chunk's queries: log-sum-exp, D, what they see
+template <int HD, int MODE>
+__device__ __forceinline__ void attn_rule_bwd_f32_body(const DeviceTables& t, const OpDesc& d, char* lds) {
+  constexpr int ROWS = kOperand / (4 * HD), CPR = HD / 4, KT = ROWS / 16, NLD = kOperand / 2048, STAGE = 2 * kOperand + kStatBytes;
+  constexpr bool OWN_Q = MODE == 1;
+  const int* ax = t.aux + d.aux0;
+  const int tq = ax[0], tk = ax[1], tc = ax[2], q_rows = ax[3], kv_rows = ax[4];
+  const int nc = d.p.n_col_tiles, gw = nc * tc, hpg = gw / HD, nq = d.p.n_q_tiles, nkv = d.p.n_kv_tiles;
+  void* const* Qt = t.ptrs + d.ptr0;
+  void* const* Kt = Qt + nq * nc;
+  void* const* Vt = Kt + nkv * nc;
+  void* const* Dt = Vt + nkv * nc;  // dO tiles
+  void* const* St = Dt + nq * nc;   // statistics per Q row tile
+  const int my_rows = OWN_Q ? q_rows : kv_rows, o_rows = OWN_Q ? kv_rows : q_rows, o_trows = OWN_Q ? tk : tq;
+  const Rule rule(t, d);
+  int h, rb;
+  head_and_rank(blockIdx.x, d.nblocks, hpg, h, rb);
+  rb = block_of_rank<kOwnRows, OWN_Q>(rule, rb, (my_rows + kOwnRows - 1) / kOwnRows, my_rows, q_rows, (int*)lds);
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 1, part = wave >> 1;
+  const Side<float, HD> Q(Qt, nc, tq, tc, q_rows, h), K(Kt, nc, tk, tc, kv_rows, h), V(Vt, nc, tk, tc, kv_rows, h), D(Dt, nc, tq, tc, q_rows, h);
+  const int row0 = rb * kOwnRows + w * 16, row = row0 + n, mine_at = min(row, my_rows - 1);
+  const bool exists = row < my_rows;
+  f32x4 m1[HD / 16], m2[HD / 16], acc[HD / 16];  // this lane's own row: Q and dO, or K and V (dV needs no V)
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) {
+    m1[j] = (OWN_Q ? Q : K).at(mine_at, 16 * j + 4 * g);
+    if (MODE != 3) m2[j] = (OWN_Q ? D : V).at(mine_at, 16 * j + 4 * g);
+    acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  auto stat = [&](int r, int which) -> float {
+    const int rt = r / tq;
+    return get_global((const float*)St[rt] + (size_t)(r - rt * tq) * (2 * hpg) + which * hpg + h);
+  };
+  const float scale = d.p.scale, slope = rule.slope(h);
+  const float my_lse = OWN_Q ? stat(mine_at, 0) : 0.f, my_D = OWN_Q ? stat(mine_at, 1) : 0.f;
+
+  int lo = 0, hi = 0;                                     // mode 1: the keys this lane's query sees
+  int w_begin = 0, w_end = 0, all_lo = 0, all_hi = 0;     // mode 1: of the wavefront
+  const int key0 = row0, key1 = min(row0 + 16, kv_rows);  // modes 2, 3: the wavefront's keys
+  int begin, end;                                         // rows of the other side that the workgroup has to do with
+  {
+    int v0 = INT_MAX, v1 = INT_MAX;  // minima of the first and of minus the one behind the last
+    if (OWN_Q) {
+      if (exists) rule.visible(row, lo, hi);
+      w_begin = wave_min(lo < hi ? lo : INT_MAX);
+      w_end = -wave_min(-hi);
+      all_lo = -wave_min(exists ? -lo : INT_MAX);
+      all_hi = wave_min(exists ? hi : INT_MAX);
+      v0 = w_begin;
+      v1 = -w_end;
+    } else {
+      const int k0 = rb * kOwnRows, k1 = min(k0 + kOwnRows, kv_rows);
+      const int first = rule.causal ? max(0, rule.k_pos0 + k0 - rule.q_pos0) : 0;
+      if (rule.spans) {
+#pragma unroll 4
+        for (int q = first + threadIdx.x; q < q_rows; q += 256) {
+          int ql, qh;
+          rule.visible(q, ql, qh);
+          if (ql < k1 && qh > k0) {
+            v0 = min(v0, q);
+            v1 = min(v1, -q - 1);
+          }
+        }
+        v0 = wave_min(v0);
+        v1 = wave_min(v1);
+      } else if (first < q_rows) {
+        v0 = first;
+        v1 = -q_rows;
+      }
+    }
+    int* const shared = (int*)lds;
+    if (lane == 0) {
+      shared[2 * wave] = v0;
+      shared[2 * wave + 1] = v1;
+    }
+    __syncthreads();
+    begin = min(min(shared[0], shared[2]), min(shared[4], shared[6]));
+    end = -min(min(shared[1], shared[3]), min(shared[5], shared[7]));
+    begin = __builtin_amdgcn_readfirstlane(begin < end ? begin & ~(ROWS - 1) : end);
+    end = __builtin_amdgcn_readfirstlane(end);
+    __syncthreads();
+  }
+
+  // the other side's chunks, K | V or Q | dO, then the statistics: of either part two stages
+  void* const* gridA = OWN_Q ? Kt : Qt;
+  void* const* gridB = OWN_Q ? Vt : Dt;
+  char* const mine = lds + part * 2 * STAGE;
+  const uint32_t mine0 = (uint32_t)(size_t)(lptr_t)lds + part * 2 * STAGE;
+  const int ct = (h * HD) / tc, cin0 = (h * HD) % tc, tid = threadIdx.x & 127;
+  float s_lse = 0.f, s_D = 0.f;  // of the chunk just issued, in registers of the part's first ROWS threads
+  int s_lo = 0, s_hi = 0;
+  auto issue = [&](int o0, int stage) {
+    const int rt = o0 / o_trows, in = o0 - rt * o_trows, trows = min(o_trows, o_rows - rt * o_trows);
+    const float* At = (const float*)sload_ptr((const void* const*)(gridA + rt * nc + ct));
+    const float* Bt = (const float*)sload_ptr((const void* const*)(gridB + rt * nc + ct));
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(mine0 + stage * STAGE + w * 1024);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) {
+      const int p = i * 128 + tid, r = p / CPR;
+      const size_t at = (size_t)min(in + r, trows - 1) * tc + cin0 + ((p % CPR) ^ (r & 15)) * 4;  // rows past the end: one that exists, hidden below
+      load_lds(At + at, dst + i * 2048);
+      load_lds(Bt + at, dst + kOperand + i * 2048);
+    }
+    if (!OWN_Q && tid < ROWS) {
+      const int q = min(o0 + tid, q_rows - 1);
+      s_lse = stat(q, 0);
+      s_D = stat(q, 1);
+      s_lo = s_hi = 0;
+      if (o0 + tid < q_rows) rule.visible(q, s_lo, s_hi);
+    }
+  };
+  uint32_t a_at[HD / 16], x_at[4][HD / 16];  // in the first stage: rows n; columns n of rows 4 g + c
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) {
+    a_at[j] = mine0 + n * (HD * 4) + ((4 * j + g) ^ n) * 16;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) x_at[c][j] = mine0 + (MODE == 3 ? kOperand : 0) + (4 * g + c) * (HD * 4) + ((4 * j + (n >> 2)) ^ (4 * g + c)) * 16 + (n & 3) * 4;
+  }
+  const float from_me = (float)(rule.q_pos0 - rule.k_pos0 + (OWN_Q ? row : -row));  // query position - key position, less the other side's index
+
+  auto chunk = [&](int o0, auto which) {
+    constexpr int at = decltype(which)::value * STAGE;
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this chunk and its statistics have arrived
+    float* const st = (float*)(mine + at + 2 * kOperand);
+    if (!OWN_Q && tid < ROWS) {
+      st[tid] = s_lse;
+      st[ROWS + tid] = s_D;
+      ((int*)st)[2 * ROWS + tid] = s_lo;
+      ((int*)st)[3 * ROWS + tid] = s_hi;
+    }
+    __syncthreads();  // ... for everybody, and everybody is done with the other stage
+    if (o0 + 2 * ROWS < end) issue(o0 + 2 * ROWS, 1 - decltype(which)::value);
+    if (o0 >= end) return;
+    bool all_see;
+    if (OWN_Q) {
+      if (o0 + ROWS <= w_begin || o0 >= w_end) return;
+      all_see = o0 >= all_lo && o0 + ROWS <= all_hi;
+    } else {
+      const int ql = ((const int*)st)[2 * ROWS + (lane & (ROWS - 1))], qh = ((const int*)st)[3 * ROWS + (lane & (ROWS - 1))];
+      if (!__any(ql < key1 && qh > key0)) return;
+      all_see = __all(ql <= key0 && qh >= row0 + 16);
+    }
+    f32x4 s[KT], dp[KT], s2[KT];
+#pragma unroll
+    for (int k = 0; k < KT; ++k) s[k] = dp[k] = s2[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) {
+      f32x4 a[KT], b[KT];
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        a[k] = *(lds_f32x4)(size_t)(a_at[j] + (at + k * 16 * (HD * 4)));
+        if (MODE != 3) b[k] = *(lds_f32x4)(size_t)(a_at[j] + (at + kOperand + k * 16 * (HD * 4)));
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          if (MODE == 3 && (j & 1)) s2[k] = mfma_f32(a[k][c], m1[j][c], s2[k]);  // chains of products enough
+          else s[k] = mfma_f32(a[k][c], m1[j][c], s[k]);
+          if (MODE != 3) dp[k] = mfma_f32(b[k][c], m2[j][c], dp[k]);
+        }
+    }
+    // element i of s[k]: row o0 + 16 k + 4 g + i of the other side
+#pragma unroll
+    for (int k = 0; k < KT; ++k) {
+      f32x4 lse = {my_lse, my_lse, my_lse, my_lse}, Dr = {my_D, my_D, my_D, my_D};
+      if (!OWN_Q) {
+        lse = *(const f32x4*)(st + 16 * k + 4 * g);
+        Dr = *(const f32x4*)(st + ROWS + 16 * k + 4 * g);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float other = (float)(o0 + 16 * k + 4 * g + i);
+        float z = (MODE == 3 ? s[k][i] + s2[k][i] : s[k][i]) * scale, th = 0.f;
+        if (rule.cap > 0.f) {
+          th = tanh_f32(z * rule.inv_cap);
+          z = rule.cap * th;
+        }
+        if (rule.slopes) z = fmaf(-slope, fabsf(OWN_Q ? from_me - other : from_me + other), z);
+        float p = __expf(z - lse[i]);
+        if (MODE != 3) p *= (dp[k][i] - Dr[i]) * scale * (1.f - th * th);
+        s[k][i] = p;
+      }
+    }
+    if (!all_see) {
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int lr = 16 * k + 4 * g + i;
+          const bool ok = OWN_Q ? o0 + lr >= lo && o0 + lr < hi : row >= ((const int*)st)[2 * ROWS + lr] && row < ((const int*)st)[3 * ROWS + lr];
+          if (!ok) s[k][i] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) acc[j] = mfma_f32(*(lds_f32)(size_t)(x_at[c][j] + (at + 16 * k * (HD * 4))), s[k][c], acc[j]);
+  };
+  const int from = begin + part * ROWS;
+  if (from < end) issue(from, 0);
+  // (both parts pass as many barriers: the second may have no last chunk)
+  for (int o0 = from; o0 - part * ROWS < end; o0 += 4 * ROWS) {
+    chunk(o0, std::integral_constant<int, 0>{});
+    if (o0 - part * ROWS + 2 * ROWS < end) chunk(o0 + 2 * ROWS, std::integral_constant<int, 1>{});
+  }
+  {  // the second part's sums by way of LDS
+    f32x4* const theirs = (f32x4*)lds;
+    __syncthreads();
+    if (part) {
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) theirs[(w * (HD / 16) + j) * 64 + lane] = acc[j];
+    }
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) acc[j] += theirs[(w * (HD / 16) + j) * 64 + lane];
+  }
+  // a weight of zero times an infinity or NaN of a row that does not matter to this one: such rows are formed again
+  float z = 0.f;
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z = fmaf(acc[j][i], 0.f, z);
+  if (__builtin_expect(__any(exists && !(z == 0.f)), 0)) return attn_bwd_by_rows<float, HD, MODE, true>(t, d, Q, K, V, D, h, gw, row0, row0 + 16, lane >> 4, 4, stat);
+  if (!exists) return;
+  float* out = (float*)d.out + (size_t)row * gw + h * HD;
+#pragma unroll
+  for (int j = 0; j < HD / 16; ++j) st4(out + 16 * j + 4 * g, acc[j]);
+}
+
 template <int HD>
-hipError_t launch(const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+__global__ void __launch_bounds__(256, 2) attn_rule_bwd_f32_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  switch (d.p.mode) {  // the three go in one launch
+    case 1: attn_rule_bwd_f32_body<HD, 1>(t, d, lds); break;
+    case 2: attn_rule_bwd_f32_body<HD, 2>(t, d, lds); break;
+    default: attn_rule_bwd_f32_body<HD, 3>(t, d, lds); break;
+  }
+}
+
+template <auto kernel>
+hipError_t launch(int lds, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  constexpr int lds = 8 * kOperand;
-  if (const hipError_t e = allow_lds(allowed, (const void*)attn_rule_f32_kernel<HD>, lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(attn_rule_f32_kernel<HD>, dim3((unsigned)max_blocks, (unsigned)b.n), dim3(256), lds, s, t, b);
+  if (const hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)max_blocks, (unsigned)b.n), dim3(256), lds, s, t, b);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int32_t attn_rule_f32_blocks(const OpDesc& d, const int32_t* aux) {
+int32_t attn_rule_f32_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   const int32_t* ax = aux + d.aux0;
-  return d.p.n_col_tiles * ax[2] / d.p.head_dim * ((ax[3] + kOwnRows - 1) / kOwnRows);
+  const int rows = cls == LC_ATTN_BWD_RULE_TILES && d.p.mode != 1 ? ax[4] : ax[3];  // keys for dK and dV, else queries
+  return d.p.n_col_tiles * ax[2] / d.p.head_dim * ((rows + kOwnRows - 1) / kOwnRows);
 }
 
-hipError_t launch_attn_rule_f32(int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
-  if (head_dim == 64) return launch<64>(t, b, max_blocks, s);
-  if (head_dim == 128) return launch<128>(t, b, max_blocks, s);
-  return hipErrorInvalidValue;
+hipError_t launch_attn_rule_f32(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+  if (head_dim != 64 && head_dim != 128) return hipErrorInvalidValue;
+  if (cls == LC_ATTN_BWD_RULE_TILES) {
+    constexpr int lds = 4 * (2 * kOperand + kStatBytes);
+    return head_dim == 64 ? launch<attn_rule_bwd_f32_kernel<64>>(lds, t, b, max_blocks, s) : launch<attn_rule_bwd_f32_kernel<128>>(lds, t, b, max_blocks, s);
+  }
+  constexpr int lds = 8 * kOperand;
+  return head_dim == 64 ? launch<attn_rule_f32_kernel<64>>(lds, t, b, max_blocks, s) : launch<attn_rule_f32_kernel<128>>(lds, t, b, max_blocks, s);
 }
 
 }  // namespace tn

@@ -535,6 +535,8 @@ tn_status build_tables(tn_executor& ex) {
           // the bf16 kernels want plain V tiles, whole heads inside one column tile and 64-row chunks of the other side inside one row tile
           vi.cls = (d.dtype == TN_BF16 && !x.p.v_trans && tc % hd == 0 && (x.p.mode == 1 ? nkv == 1 || tk % 64 == 0 : nq == 1 || tq % 64 == 0))
                        ? (int8_t)(LC_ATTN_BWD_RULE_BF16 + 4 * (x.p.mode - 1) + rule_kernel(x.p)) : (int8_t)LC_ATTN_BWD_RULE;
+          if (d.dtype == TN_F32 && !x.p.v_trans && tc % hd == 0 && (x.p.mode == 1 ? nkv == 1 || tk % (2048 / hd) == 0 : nq == 1 || tq % (2048 / hd) == 0))
+            vi.cls = LC_ATTN_BWD_RULE_TILES;
           vi.head_dim = (int16_t)hd;
           vi.flops = (x.p.mode == 3 ? 4.0 : 6.0) * visible_pairs(q_rows, kv_rows, x.p) * (double)(nc * tc);
           vi.bytes = (2.0 * q_rows + 2.0 * kv_rows) * nc * tc * elem_bytes(d.dtype);
@@ -704,7 +706,8 @@ int family_of(int cls) {
     case LC_ATTN_BWD_BF16_DV:
     case LC_ATTN_RULE_F32:
     case LC_ATTN_RULE_F32_TILES:
-    case LC_ATTN_BWD_RULE: return 1;
+    case LC_ATTN_BWD_RULE:
+    case LC_ATTN_BWD_RULE_TILES: return 1;
     default: return is_attn_rule_bf16(cls) ? 1 : 2;
   }
 }

@@ -91,6 +91,7 @@ enum LaunchClass {
   LC_ATTN_RULE_F32,  // attention with a score rule or finished rows, fp32 products
   LC_ATTN_RULE_F32_TILES, // the same where a chunk of keys of a head lies inside one tile
   LC_ATTN_BWD_RULE,  // its gradients, fp32 products
+  LC_ATTN_BWD_RULE_TILES, // the same where a chunk of the other side's rows of a head lies inside one tile
   LC_ATTN_RULE_BF16, // attention with a score rule or finished rows, bf16 products: plus kRuleHasCap and kRuleHasSlopes
   LC_ATTN_RULE_BF16_LAST = LC_ATTN_RULE_BF16 + 3,
   LC_ATTN_BWD_RULE_BF16, // its gradients: plus 4 for dK, 8 for dV, and the same
@@ -246,9 +247,9 @@ inline int32_t head_walk(int64_t rows, int32_t heads, int32_t head_dim) {
 int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux);
 hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
-// LC_ATTN_RULE_F32_TILES: attn_rule_f32.hip.
-int32_t attn_rule_f32_blocks(const OpDesc& d, const int32_t* aux);
-hipError_t launch_attn_rule_f32(int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
+// LC_ATTN_RULE_F32_TILES and LC_ATTN_BWD_RULE_TILES: attn_rule_f32.hip.
+int32_t attn_rule_f32_blocks(int cls, const OpDesc& d, const int32_t* aux);
+hipError_t launch_attn_rule_f32(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
 // LC_ATTN_F32 and LC_ATTN_RULE_F32 (reverse == false), LC_ATTN_BWD and LC_ATTN_BWD_RULE: attn_f32.hip.
 hipError_t launch_attn_f32(bool reverse, bool rule, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks,

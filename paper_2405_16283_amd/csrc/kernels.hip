@@ -1405,7 +1405,8 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
     case LC_ATTN_STATS: return cdiv((int64_t)d.rows * (d.p.n_col_tiles * aux[d.aux0 + 2] / d.p.head_dim), 16);
     case LC_ATTN_JOIN_FEW: return d.rows * (d.cols / d.p.head_dim);
     case LC_ATTN_LSE: return cdiv((int64_t)d.rows * d.cols, 256);
-    case LC_ATTN_RULE_F32_TILES: return attn_rule_f32_blocks(d, aux);
+    case LC_ATTN_BWD_RULE_TILES:
+    case LC_ATTN_RULE_F32_TILES: return attn_rule_f32_blocks(cls, d, aux);
     case LC_ATTN_RULE_F32:
     case LC_ATTN_F32: {
       const int gw = d.p.n_col_tiles * aux[d.aux0 + 2];
@@ -1553,7 +1554,8 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
     case LC_HEAD_GAIN_EIGHTS:
     case LC_COL_SUM: return launch_heads(cls, dtype, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE: return launch_attn_f32(true, true, dtype, head_dim, t, b, max_blocks, s);
-    case LC_ATTN_RULE_F32_TILES: return launch_attn_rule_f32(head_dim, t, b, max_blocks, s);
+    case LC_ATTN_BWD_RULE_TILES:
+    case LC_ATTN_RULE_F32_TILES: return launch_attn_rule_f32(cls, head_dim, t, b, max_blocks, s);
     case LC_ATTN_RULE_F32: return launch_attn_f32(false, true, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BWD: return launch_attn_f32(true, false, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_F32: return launch_attn_f32(false, false, dtype, head_dim, t, b, max_blocks, s);

@@ -68,12 +68,13 @@ def attention(q, k, v, head_dim, scale, ok, cap=0.0, slopes=None, q_pos0=0, k_po
     return torch.cat(outs, 1), torch.stack(lses, 1)
 
 
-def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, slopes=None, q_pos0=0, k_pos0=0, do=None, rounded_o=True):
+def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, slopes=None, q_pos0=0, k_pos0=0, do=None, rounded_o=True, cap_sized=True):
     """How far correct results may lie from the exact ones, element by element: {"o", "lse"} and with `do` {"dq", "dk", "dv"}.
 
     Counted are the roundings a kernel makes: of stored results (`storage`: half a step relative to the value, 2^-8 or 2^-24), of weights
     and their gradients where they enter a product (`products`: 2^-8 for bf16 products, 0 for fp32), and those of fp32 arithmetic: of
     a score, one unit (2^-24) per term of its sum and a few more for scaling, cap, bias and the exponential; of a sum over n rows, n units;
+    a capped score's units are of its own size and, cap_sized, of the cap's (it is formed as cap - 2 cap / (1 + exp(2 z / cap))).
     O enters the reverse pass rounded to storage, or (rounded_o False) as it was before.  Below 2^-126, the smallest normal number, a weight, its gradient or a result may be zero."""
     u, tiny = 2.0 ** -24, 2.0 ** -126
     out = {n: [] for n in ("o", "lse", "dq", "dk", "dv")}
@@ -84,7 +85,7 @@ def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, s
         slope = None if slopes is None else slopes[h]
         raw = (Q.abs() @ K.abs().T) * scale
         s = scores(Q, K, scale, cap, slope, q_pos0, k_pos0)
-        size = s.abs() + cap
+        size = s.abs() + (cap if cap_sized else 0.0)
         if slope is not None:
             size = size + (s - scores(Q, K, scale, cap)).abs()
         e = u * ((head_dim + 8) * raw + 8 * size + 8)            # of a score

@@ -220,6 +220,10 @@ inline bool join_few(const OpDesc& d) {
   return d.n_in >= 16 && (int64_t)d.rows * d.cols <= 512 * 1024 && hd % 4 == 0 && hd <= 1024 && d.p.hpg % 2 == 0 && d.p.col0 % hd == 0 && d.cols % hd == 0;
 }
 enum { kRuleHasCap = 1, kRuleHasSlopes = 2 };  // kernels of their own
+// The largest cap that the bf16 kernels take: they form a capped score as cap - 2 cap / (1 + exp(2 z / cap)), of which cap * 2^-22 and a little
+// is lost: 2^-12 of a weight here, and more than its rounding to bf16 from some ten times as much.  Larger ones go to attn_f32.hip (1024 causal
+// rows of 32 heads of 128: 295 us instead of 38, gradients 772 instead of 134; a cap is some tens where it is used at all).
+constexpr float kRuleCapMost = 1024.f;
 // LC_ATTN_RULE_BF16 to LC_ATTN_BWD_RULE_BF16_LAST: attn_rule.hip.
 inline bool is_attn_rule_bf16(int cls) { return cls >= LC_ATTN_RULE_BF16 && cls <= LC_ATTN_BWD_RULE_BF16_LAST; }
 int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux);

@@ -42,7 +42,8 @@ static tn_status validate_rule(const TaskGraph& g, const char* name, const tn_op
   if (!(p.score_cap == 0.f || (p.score_cap >= 1e-6f && p.score_cap <= 1e6f))) return fail(TN_ERR_SHAPE, "%s: score_cap must be 0 or lie in 1e-6 .. 1e6", name);
   if (!has_rule(p) && !finished) return TN_OK;
   // caps and slopes are of scores that are scaled already, and the kernels count positions in 32 bits
-  if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(TN_ERR_SHAPE, "%s: a score rule and finished rows need a positive scale", name);
+  // (the reverse pass divides log-sum-exps by the scale)
+  if (!(p.scale >= 1e-20f && p.scale <= 1e20f)) return fail(TN_ERR_SHAPE, "%s: a score rule and finished rows need a scale in 1e-20 .. 1e20", name);
   if (p.q_pos0 < 0 || p.k_pos0 < 0 || p.q_pos0 > (1 << 30) || p.k_pos0 > (1 << 30))
     return fail(TN_ERR_SHAPE, "%s: with a score rule or finished rows q_pos0 and k_pos0 lie in 0 .. 2^30", name);
   if (p.slopes) {

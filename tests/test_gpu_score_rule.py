@@ -68,6 +68,9 @@ CASES = {
     "transposed": dict(rows=140, keys=140, heads=2, hd=64, v_trans=1, cap=8.0, spans=_documents(140, [50])),
     "odd tiles": dict(rows=130, keys=171, heads=3, hd=64, row_tile=50, q_pos0=41, cap=8.0, slopes=1, spans=_window(130, 90, first=41)),
     "tiles of sixteen": dict(rows=60, keys=75, heads=2, hd=128, row_tile=16, causal=0, cap=8.0, spans=_holes(60, 75, 4)),
+    "capped at a thousand": dict(rows=130, keys=130, heads=2, hd=128, cap=1000.0, std=4.0),
+    "capped at half a million": dict(rows=130, keys=130, heads=2, hd=64, cap=5e5, std=4.0),
+    "capped at a million, slopes": dict(rows=70, keys=70, heads=2, hd=128, cap=1e6, slopes=1),
     "more blocks than compute units": dict(rows=1100, keys=1100, heads=8, hd=64, spans=_documents(1100, [300, 310, 900])),
     "more of odd heads": dict(rows=1000, keys=300, heads=9, hd=64, causal=0, slopes=1, k_pos0=100),
     "blocks without an order": dict(rows=8300, keys=40, heads=1, hd=64, causal=0, cap=6.0, spans=_holes(8300, 40, 3)),
@@ -148,7 +151,7 @@ class Case:
         c, b = self.c, self.dtype == "bf16"
         t = torch.tensor
         x = H.attention_bounds(t(self.q), t(self.k), t(self.v), c["hd"], self.scale, self.ok, 2.0 ** (-8 if b else -24), 2.0 ** -8 if b else 0.0, self.cap,
-                               self.slopes, c["q_pos0"], c["k_pos0"], t(self.do) if grad else None, rounded_o)
+                               self.slopes, c["q_pos0"], c["k_pos0"], t(self.do) if grad else None, rounded_o, cap_sized=b and self.cap <= 1024.0)
         return {n: a.numpy() for n, a in x.items()}
 
 

@@ -82,7 +82,7 @@ def test_score_rules(g):
                      ([q, k, k], dict(spans=1)), ([q, k, k, slopes], dict(spans=1)), ([q, k, k, spans], dict(slopes=1)), ([q, k, k, spans, slopes], dict(slopes=1, spans=1)),
                      ([q, k, k, g.inp(10, 2)], dict(spans=1)), ([q, k, k, g.inp(9, 2, B.TN_I32)], dict(spans=1)), ([q, k, k, g.inp(10, 1, B.TN_I32)], dict(spans=1)),
                      ([q, k, k, g.inp(1, 3)], dict(slopes=1)), ([q, k, k, slopes], {}), ([q, k, k], dict(score_cap=5.0, scale=0.0)),
-                     ([q, k, k], dict(score_cap=5.0, scale=-1.0)), ([q, k, k], dict(score_cap=5.0, scale=float("nan"))), ([q, k, k], dict(score_cap=5.0, q_pos0=-1)),
+                     ([q, k, k], dict(score_cap=5.0, scale=-1.0)), ([q, k, k], dict(score_cap=5.0, scale=float("nan"))), ([q, k, k], dict(score_cap=5.0, scale=1e-21)), ([q, k, k], dict(score_cap=5.0, scale=1e21)), ([q, k, k], dict(score_cap=5.0, q_pos0=-1)),
                      ([q, k, k], dict(score_cap=5.0, k_pos0=2 ** 30 + 1)), ([q, k, k, spans], dict(spans=1, n_q_tiles=-1)), ([q, k, k, spans], dict(spans=1, n_q_tiles=2 ** 31 - 1)),
                      ([q, g.inp(20, 128, B.TN_I32), k, spans], dict(spans=1))):
         _refused(g, A, ins, 10, 132, **{**good, **bad})

@@ -40,6 +40,13 @@ __device__ __forceinline__ int swizzle(int row) {
   return HD == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 2) << 1) | ((row >> 2) & 3);
 }
 
+// what is the same in every lane, where the compiler does not see it
+__device__ __forceinline__ const void* const* uniform(const void* const* p) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (const void* const*)((uint64_t)hi << 32 | lo);
+}
+
 // A lane's own row as MFMA operand: 16-byte pieces 2 s + g of head h.  One tile: its address is the wavefront's.
 template <int HD>
 __device__ __forceinline__ void load_own(void* const* tiles, int n_tiles, int nc, int trows, int tc, int row, int h, int g, bf16x8 (&v)[HD / 16]) {
@@ -291,13 +298,10 @@ constexpr int kBwdStats = 4 * kRuleKeys * 4;  // of a stage's queries (modes 2, 
 constexpr int attn_rule_bwd_lds(int hd) { return 2 * (2 * kRuleKeys * hd * 2 + kBwdStats); }
 
 template <int HD, int MODE, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, Batch b) {
-  const OpDesc& d = t.descs[b.at(blockIdx.y)];
-  if ((int)blockIdx.x >= d.nblocks) return;
+__device__ __forceinline__ void attn_rule_bwd_body(const DeviceTables& t, const OpDesc& d, char* lds) {
   constexpr bool OWN_Q = MODE == 1;
   constexpr int CH = kRuleKeys, CPR = HD / 8, ABYTES = CH * HD * 2, STAGE = 2 * ABYTES + kBwdStats;
   constexpr int NLD = CH * CPR / 256, SUBS = MODE == 3 || HD == 64 ? 2 : 1;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int* ax = t.aux + d.aux0;
   const int tq = ax[0], tk = ax[1], tc = ax[2], q_rows = ax[3], kv_rows = ax[4];
   const int nc = d.p.n_col_tiles, gw = nc * tc, hpg = gw / HD, nq = d.p.n_q_tiles, nkv = d.p.n_kv_tiles;
@@ -396,11 +400,11 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
     if (nrt != rt) {
       rt = nrt;
       if (!OWN_Q) {
-        stats = (const float*)sload_ptr((const void* const*)(St + rt)) + h;
-        if (rule.spans) spans = (const int2_t*)sload_ptr((const void* const*)(rule.spans + rt));
+        stats = (const float*)sload_ptr(uniform((const void* const*)(St + rt))) + h;
+        if (rule.spans) spans = (const int2_t*)sload_ptr(uniform((const void* const*)(rule.spans + rt)));
       }
-      At = (const bf16_t*)sload_ptr((const void* const*)(gridA + rt * nc + ct));
-      Bt = (const bf16_t*)sload_ptr((const void* const*)(gridB + rt * nc + ct));
+      At = (const bf16_t*)sload_ptr(uniform((const void* const*)(gridA + rt * nc + ct)));
+      Bt = (const bf16_t*)sload_ptr(uniform((const void* const*)(gridB + rt * nc + ct)));
       trows = min(o_trows, o_rows - rt * o_trows);
     }
     const int in = o0 - rt * o_trows;
@@ -584,6 +588,20 @@ __global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, B
           make_uint2(f2bf2(acc[i][4 * a] * oscale, acc[i][4 * a + 1] * oscale), f2bf2(acc[i][4 * a + 2] * oscale, acc[i][4 * a + 3] * oscale));
 }
 
+// The three gradients of an attention block are ready together, and go in one launch: one's last workgroups run beside the next one's first.
+// Apart and so, 32 heads of 128 with a cap: 4096 rows of three documents 386 and 360 us, of one 1304 and 1276; 8 heads of 1000 rows 121 and 47.
+template <int HD, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(256, 2) attn_rule_bwd_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  switch (d.p.mode) {
+    case 1: attn_rule_bwd_body<HD, 1, CAP, SLOPES>(t, d, lds); break;
+    case 2: attn_rule_bwd_body<HD, 2, CAP, SLOPES>(t, d, lds); break;
+    default: attn_rule_bwd_body<HD, 3, CAP, SLOPES>(t, d, lds); break;
+  }
+}
+
 template <auto kernel>
 hipError_t launch(int threads, int lds, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
@@ -604,19 +622,15 @@ hipError_t launch_forward(int rule, const DeviceTables& t, const Batch& b, int32
   }
 }
 
-template <int HD, int MODE>
+template <int HD>
 hipError_t launch_reverse(int rule, const DeviceTables& t, const Batch& b, int32_t n, hipStream_t s) {
   constexpr int lds = attn_rule_bwd_lds(HD);
   switch (rule) {
-    case 0: return launch<attn_rule_bwd_kernel<HD, MODE, false, false>>(256, lds, t, b, n, s);
-    case kRuleHasCap: return launch<attn_rule_bwd_kernel<HD, MODE, true, false>>(256, lds, t, b, n, s);
-    case kRuleHasSlopes: return launch<attn_rule_bwd_kernel<HD, MODE, false, true>>(256, lds, t, b, n, s);
-    default: return launch<attn_rule_bwd_kernel<HD, MODE, true, true>>(256, lds, t, b, n, s);
+    case 0: return launch<attn_rule_bwd_kernel<HD, false, false>>(256, lds, t, b, n, s);
+    case kRuleHasCap: return launch<attn_rule_bwd_kernel<HD, true, false>>(256, lds, t, b, n, s);
+    case kRuleHasSlopes: return launch<attn_rule_bwd_kernel<HD, false, true>>(256, lds, t, b, n, s);
+    default: return launch<attn_rule_bwd_kernel<HD, true, true>>(256, lds, t, b, n, s);
   }
-}
-template <int HD>
-hipError_t launch_reverse(int mode, int rule, const DeviceTables& t, const Batch& b, int32_t n, hipStream_t s) {
-  return mode == 1 ? launch_reverse<HD, 1>(rule, t, b, n, s) : mode == 2 ? launch_reverse<HD, 2>(rule, t, b, n, s) : launch_reverse<HD, 3>(rule, t, b, n, s);
 }
 
 }  // namespace
@@ -629,9 +643,8 @@ int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux) {
 
 hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
   if (cls >= LC_ATTN_BWD_RULE_BF16) {
-    const int mode = 1 + (cls - LC_ATTN_BWD_RULE_BF16) / 4, rule = (cls - LC_ATTN_BWD_RULE_BF16) % 4;
-    if (head_dim == 64) return launch_reverse<64>(mode, rule, t, b, max_blocks, s);
-    if (head_dim == 128) return launch_reverse<128>(mode, rule, t, b, max_blocks, s);
+    if (head_dim == 64) return launch_reverse<64>(cls - LC_ATTN_BWD_RULE_BF16, t, b, max_blocks, s);
+    if (head_dim == 128) return launch_reverse<128>(cls - LC_ATTN_BWD_RULE_BF16, t, b, max_blocks, s);
     return hipErrorInvalidValue;
   }
   if (head_dim == 64) return launch_forward<64>(cls - LC_ATTN_RULE_BF16, t, b, max_blocks, s);

@@ -534,7 +534,7 @@ tn_status build_tables(tn_executor& ex) {
           add_rule(x.p, 2 * (nq + nkv) * nc + nq);
           // the bf16 kernels want plain V tiles, whole heads inside one column tile and 64-row chunks of the other side inside one row tile
           vi.cls = (d.dtype == TN_BF16 && x.p.score_cap <= kRuleCapMost && !x.p.v_trans && tc % hd == 0 && (x.p.mode == 1 ? nkv == 1 || tk % 64 == 0 : nq == 1 || tq % 64 == 0))
-                       ? (int8_t)(LC_ATTN_BWD_RULE_BF16 + 4 * (x.p.mode - 1) + rule_kernel(x.p)) : (int8_t)LC_ATTN_BWD_RULE;
+                       ? (int8_t)(LC_ATTN_BWD_RULE_BF16 + rule_kernel(x.p)) : (int8_t)LC_ATTN_BWD_RULE;
           if (d.dtype == TN_F32 && !x.p.v_trans && tc % hd == 0 && (x.p.mode == 1 ? nkv == 1 || tk % (2048 / hd) == 0 : nq == 1 || tq % (2048 / hd) == 0))
             vi.cls = LC_ATTN_BWD_RULE_TILES;
           vi.head_dim = (int16_t)hd;

@@ -94,8 +94,8 @@ enum LaunchClass {
   LC_ATTN_BWD_RULE_TILES, // the same where a chunk of the other side's rows of a head lies inside one tile
   LC_ATTN_RULE_BF16, // attention with a score rule or finished rows, bf16 products: plus kRuleHasCap and kRuleHasSlopes
   LC_ATTN_RULE_BF16_LAST = LC_ATTN_RULE_BF16 + 3,
-  LC_ATTN_BWD_RULE_BF16, // its gradients: plus 4 for dK, 8 for dV, and the same
-  LC_ATTN_BWD_RULE_BF16_LAST = LC_ATTN_BWD_RULE_BF16 + 11,
+  LC_ATTN_BWD_RULE_BF16, // its gradients: plus the same
+  LC_ATTN_BWD_RULE_BF16_LAST = LC_ATTN_BWD_RULE_BF16 + 3,
   LC_ATTN_STATS,     // their statistics from O, dO and the log-sum-exp
   LC_ATTN_JOIN,      // combine with finish 1
   LC_ATTN_JOIN_FEW,  // the same for few rows over many partials

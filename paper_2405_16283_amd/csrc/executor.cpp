@@ -377,7 +377,7 @@ tn_status build_tables(tn_executor& ex) {
       case TN_OP_HEAD_ROPE_BWD: {
         const bool back = x.op_kind == TN_OP_HEAD_ROPE_BWD;
         const tn_tensor_desc& xd = odesc(back ? 1 : 0);
-        vi.cls = !back ? LC_HEAD_ROPE : x.p.mode ? LC_HEAD_GAIN : LC_HEAD_ROPE_BWD;
+        vi.cls = back ? LC_HEAD_ROPE_BWD : LC_HEAD_ROPE;
         vi.bytes = (back ? 2.0 : 1.0) * tensor_bytes(xd) + (double)x.bytes;
         const int rd = x.p.rotary_dim ? x.p.rotary_dim : x.p.head_dim;
         const float scaled[4] = {x.p.rope_factor, x.p.rope_low, x.p.rope_high, x.p.rope_base};

@@ -145,9 +145,7 @@ __device__ __forceinline__ float load_reverse(const Head& s, const T* dy, const 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) head_rope_bwd_kernel(DeviceTables t, Batch b) {
-  const OpDesc& d = t.descs[b.at(blockIdx.y)];
-  if ((int)blockIdx.x >= d.nblocks) return;
+__device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& d) {
   const Head s(t, d);
   const int lane = threadIdx.x & 63;
   for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * 4) {
@@ -183,11 +181,8 @@ __global__ void __launch_bounds__(256) head_rope_bwd_kernel(DeviceTables t, Batc
 // Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every fourth (row, head) of them and keeps its
 // sums in registers; the four are added in order.
 template <typename T>
-__global__ void __launch_bounds__(256) head_gain_kernel(DeviceTables t, Batch b) {
-  const OpDesc& d = t.descs[b.at(blockIdx.y)];
-  if ((int)blockIdx.x >= d.nblocks) return;
+__device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d, float (*part)[1024]) {
   const Head s(t, d);
-  __shared__ float part[4][1024];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
   float ga[kPer], gb[kPer];
@@ -216,6 +211,16 @@ __global__ void __launch_bounds__(256) head_gain_kernel(DeviceTables t, Batch b)
   __syncthreads();
   float* o = (float*)d.out + (size_t)block * s.head_dim;
   for (int c = threadIdx.x; c < s.head_dim; c += 256) o[c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+}
+
+// Both gradients go in one launch.
+template <typename T>
+__global__ void __launch_bounds__(256) head_rope_bwd_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  __shared__ float part[4][1024];
+  if (d.p.mode) head_gain<T>(t, d, part);
+  else head_input<T>(t, d);
 }
 
 // ---- heads of a multiple of 16 elements, pairs that come in eights ---------------------------------
@@ -316,9 +321,9 @@ __device__ __forceinline__ void rotate8(float (&u)[8], float (&v)[8], const floa
 struct Walk {
   int row, h0, h1;
   bool any;
-  __device__ Walk(const Head& s, int lanes) {
+  __device__ Walk(const Head& s, int lanes, int threads) {
     const int walk = s.ax[kHeadWalk], runs = (s.heads + walk - 1) / walk;
-    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+    const int64_t id = ((int64_t)blockIdx.x * threads + threadIdx.x) / lanes;
     any = id < (int64_t)s.rows * runs;
     row = any ? (int)(id % s.rows) : 0;
     h0 = any ? (int)(id / s.rows) * walk : 0;
@@ -332,7 +337,7 @@ __global__ void __launch_bounds__(256) head_rope_eights_kernel(DeviceTables t, B
   if ((int)blockIdx.x >= d.nblocks) return;
   const Head s(t, d);
   const Eights e(s);
-  const Walk at(s, e.lanes);
+  const Walk at(s, e.lanes, 256);
   const bool on = e.there && at.any;
   const T* x = (const T*)t.ptrs[d.ptr0] + (size_t)at.row * s.cols;
   T* o = (T*)d.out + (size_t)at.row * s.cols;
@@ -381,13 +386,12 @@ __global__ void __launch_bounds__(256) head_rope_eights_kernel(DeviceTables t, B
   }
 }
 
+constexpr int kBwdThreads = 512;
 template <typename T>
-__global__ void __launch_bounds__(256) head_rope_bwd_eights_kernel(DeviceTables t, Batch b) {
-  const OpDesc& d = t.descs[b.at(blockIdx.y)];
-  if ((int)blockIdx.x >= d.nblocks) return;
+__device__ __forceinline__ void head_input_eights(const DeviceTables& t, const OpDesc& d) {
   const Head s(t, d);
   const Eights e(s);
-  const Walk at(s, e.lanes);
+  const Walk at(s, e.lanes, kBwdThreads);
   const bool on = e.there && at.any;
   const T* dy = (const T*)t.ptrs[d.ptr0] + (size_t)at.row * s.cols;
   const T* x = (const T*)t.ptrs[d.ptr0 + 1] + (size_t)at.row * s.cols;
@@ -446,16 +450,12 @@ __global__ void __launch_bounds__(256) head_rope_bwd_eights_kernel(DeviceTables 
 // of the input, formed from the same operands, leaves its last ones in the caches.  16384 rows of 32 heads of 128, bf16: 55 us (268
 // MB, 4.9 TB/s), from the first row on 63.  64 rows: 18 us, sixteen heads one behind the other; with 256 threads, which take 32,
 // 23; with 1024 17, but three heads of 64 in fp32 14 instead of 9, since registers spill.
-constexpr int kGainThreads = 512;
 template <typename T>
-__global__ void __launch_bounds__(kGainThreads) head_gain_eights_kernel(DeviceTables t, Batch b) {
-  const OpDesc& d = t.descs[b.at(blockIdx.y)];
-  if ((int)blockIdx.x >= d.nblocks) return;
+__device__ __forceinline__ void head_gain_eights(const DeviceTables& t, const OpDesc& d, float (*part)[1024]) {
   const Head s(t, d);
   const Eights e(s);
-  __shared__ float part[kGainThreads / 64][1024];
   const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
-  const int groups = kGainThreads / e.lanes, group = threadIdx.x / e.lanes;
+  const int groups = kBwdThreads / e.lanes, group = threadIdx.x / e.lanes;
   const int per_row = max(1, groups / kGainRows);  // groups that share a row
   float ga[8] = {}, gb[8] = {};
   for (int r = group / per_row; r < n; r += groups / per_row) {
@@ -511,12 +511,22 @@ __global__ void __launch_bounds__(kGainThreads) head_gain_eights_kernel(DeviceTa
   }
   __syncthreads();
   float* o = (float*)d.out + (size_t)block * s.head_dim;
-  for (int c = threadIdx.x; c < s.head_dim; c += kGainThreads) {
+  for (int c = threadIdx.x; c < s.head_dim; c += kBwdThreads) {
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kGainThreads / 64; ++w) sum += part[w][c];
+    for (int w = 0; w < kBwdThreads / 64; ++w) sum += part[w][c];
     o[c] = sum;
   }
+}
+
+// Both gradients go in one launch.
+template <typename T>
+__global__ void __launch_bounds__(kBwdThreads) head_rope_bwd_eights_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  __shared__ float part[kBwdThreads / 64][1024];
+  if (d.p.mode) head_gain_eights<T>(t, d, part);
+  else head_input_eights<T>(t, d);
 }
 
 // Sum of all rows of the operands: a workgroup per 32 columns, eight threads to a column, each every eighth row; their sums are
@@ -549,14 +559,16 @@ __global__ void __launch_bounds__(256) col_sum_kernel(DeviceTables t, Batch b) {
 int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   const int32_t* ax = aux + d.aux0;
   const int64_t heads = cls == LC_COL_SUM ? 0 : ax[kHeadCols] / d.p.head_dim;
+  auto walks = [&](int64_t threads) {
+    return (int32_t)((ax[kHeadRows] * ((heads + ax[kHeadWalk] - 1) / ax[kHeadWalk]) * head_lanes(d.p.head_dim) + threads - 1) / threads);
+  };
   switch (cls) {
-    case LC_HEAD_ROPE:
-    case LC_HEAD_ROPE_BWD: return (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + 3) / 4, kGenericBlocks);
-    case LC_HEAD_ROPE_EIGHTS:
-    case LC_HEAD_ROPE_BWD_EIGHTS:
-      return (int32_t)((ax[kHeadRows] * ((heads + ax[kHeadWalk] - 1) / ax[kHeadWalk]) * head_lanes(d.p.head_dim) + 255) / 256);
-    case LC_HEAD_GAIN:
-    case LC_HEAD_GAIN_EIGHTS: return d.rows;
+    case LC_HEAD_ROPE_BWD:
+      if (d.p.mode) return d.rows;  // sums of the gain's gradient
+      [[fallthrough]];
+    case LC_HEAD_ROPE: return (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + 3) / 4, kGenericBlocks);
+    case LC_HEAD_ROPE_EIGHTS: return walks(256);
+    case LC_HEAD_ROPE_BWD_EIGHTS: return d.p.mode ? d.rows : walks(kBwdThreads);
     default: return (d.cols + 31) / 32;
   }
 }
@@ -572,12 +584,10 @@ hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& 
   switch (cls) {
     case LC_HEAD_ROPE: TN_LAUNCH(head_rope_kernel); break;
     case LC_HEAD_ROPE_BWD: TN_LAUNCH(head_rope_bwd_kernel); break;
-    case LC_HEAD_GAIN: TN_LAUNCH(head_gain_kernel); break;
     case LC_HEAD_ROPE_EIGHTS: TN_LAUNCH(head_rope_eights_kernel); break;
-    case LC_HEAD_ROPE_BWD_EIGHTS: TN_LAUNCH(head_rope_bwd_eights_kernel); break;
-    case LC_HEAD_GAIN_EIGHTS:
-      if (bf) hipLaunchKernelGGL(head_gain_eights_kernel<bf16_t>, grid, dim3(kGainThreads), 0, s, t, b);
-      else hipLaunchKernelGGL(head_gain_eights_kernel<float>, grid, dim3(kGainThreads), 0, s, t, b);
+    case LC_HEAD_ROPE_BWD_EIGHTS:
+      if (bf) hipLaunchKernelGGL(head_rope_bwd_eights_kernel<bf16_t>, grid, dim3(kBwdThreads), 0, s, t, b);
+      else hipLaunchKernelGGL(head_rope_bwd_eights_kernel<float>, grid, dim3(kBwdThreads), 0, s, t, b);
       break;
     case LC_COL_SUM: hipLaunchKernelGGL(col_sum_kernel, grid, wg, 0, s, t, b); break;
     default: return hipErrorInvalidValue;

@@ -82,11 +82,9 @@ enum LaunchClass {
   LC_SOFTMAX_STAT,   // row maximum and sum of exponentials over the score tiles of a row block
   LC_SOFTMAX_APPLY,  // probabilities of one score tile
   LC_HEAD_ROPE,      // norm and rotation of heads, any size
-  LC_HEAD_ROPE_BWD,  // gradient of their input
-  LC_HEAD_GAIN,      // sums of their gain's gradient
-  LC_HEAD_ROPE_EIGHTS, // the three for heads of a multiple of 16 elements
+  LC_HEAD_ROPE_BWD,  // gradients of their input and their gain
+  LC_HEAD_ROPE_EIGHTS, // both for heads of a multiple of 16 elements
   LC_HEAD_ROPE_BWD_EIGHTS,
-  LC_HEAD_GAIN_EIGHTS,
   LC_COL_SUM,
   LC_ATTN_RULE_F32,  // attention with a score rule or finished rows, fp32 products
   LC_ATTN_RULE_F32_TILES, // the same where a chunk of keys of a head lies inside one tile
@@ -229,7 +227,7 @@ inline bool is_attn_rule_bf16(int cls) { return cls >= LC_ATTN_RULE_BF16 && cls 
 int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux);
 hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
-// LC_HEAD_ROPE to LC_COL_SUM: heads.hip.  Auxiliary integers of the first three (of LC_COL_SUM: rows per operand):
+// LC_HEAD_ROPE to LC_COL_SUM: heads.hip.  Auxiliary integers of all but the last (of LC_COL_SUM: rows per operand):
 enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadWalk, kHeadAux };
 constexpr int kGainRows = 32;  // rows to a sum of the gain's gradient
 // Heads of a multiple of 16 elements whose pairs come in eights go to the kernels for those: 16 elements to a lane, a head to a power of

@@ -1397,10 +1397,8 @@ int32_t blocks_for(int cls, const OpDesc& d, const int32_t* aux) {
       return rope_whole_heads(d) ? cdiv((int64_t)d.rows * (d.p.head_dim / 8), 256) : cdiv((int64_t)d.rows * (d.cols / 2), 256);
     case LC_HEAD_ROPE:
     case LC_HEAD_ROPE_BWD:
-    case LC_HEAD_GAIN:
     case LC_HEAD_ROPE_EIGHTS:
     case LC_HEAD_ROPE_BWD_EIGHTS:
-    case LC_HEAD_GAIN_EIGHTS:
     case LC_COL_SUM: return head_blocks(cls, d, aux);
     case LC_ATTN_STATS: return cdiv((int64_t)d.rows * (d.p.n_col_tiles * aux[d.aux0 + 2] / d.p.head_dim), 16);
     case LC_ATTN_JOIN_FEW: return d.rows * (d.cols / d.p.head_dim);
@@ -1548,10 +1546,8 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
 #undef TN_LAUNCH_ATTN_BWD
     case LC_HEAD_ROPE:
     case LC_HEAD_ROPE_BWD:
-    case LC_HEAD_GAIN:
     case LC_HEAD_ROPE_EIGHTS:
     case LC_HEAD_ROPE_BWD_EIGHTS:
-    case LC_HEAD_GAIN_EIGHTS:
     case LC_COL_SUM: return launch_heads(cls, dtype, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE: return launch_attn_f32(true, true, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE_TILES:

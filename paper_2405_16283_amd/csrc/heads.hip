@@ -120,43 +120,55 @@ __global__ void __launch_bounds__(256) head_rope_kernel(DeviceTables t, Batch b)
   }
 }
 
+// sines and cosines of this lane's pairs in a row at `pos`
+template <int PER>
+__device__ __forceinline__ void angles(const Head& s, double pos, int lane, float (&sn)[PER], float (&cs)[PER]) {
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    sn[k] = 0.f;
+    cs[k] = 1.f;
+    if (s.pairs.turns(lane + 64 * k)) turn(pos, s.turns[lane + 64 * k], sn[k], cs[k]);
+  }
+}
+
 // The reverse of a head in registers: u (the inverse rotation of dY) and x of this lane's pairs, and 1 / rms.
-template <typename T>
-__device__ __forceinline__ float load_reverse(const Head& s, const T* dy, const T* x, double pos, int lane, float (&ua)[kPer], float (&ub)[kPer],
-                                              float (&xa)[kPer], float (&xb)[kPer]) {
+template <typename T, int PER>
+__device__ __forceinline__ float load_reverse(const Head& s, const T* dy, const T* x, const float (&sn)[PER], const float (&cs)[PER], int lane, float (&ua)[PER],
+                                              float (&ub)[PER], float (&xa)[PER], float (&xb)[PER]) {
   float ss = 0.f;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
+  for (int k = 0; k < PER; ++k) {
     const int i = lane + 64 * k;
     ua[k] = ub[k] = xa[k] = xb[k] = 0.f;
     if (i >= s.head_dim / 2) continue;
     int ea, eb;
     s.pairs.elements(i, ea, eb);
-    xa[k] = ld(x + ea);
-    xb[k] = ld(x + eb);
+    xa[k] = ld_global(x + ea);
+    xb[k] = ld_global(x + eb);
     ss += xa[k] * xa[k] + xb[k] * xb[k];
-    const float a = ld(dy + ea), c = ld(dy + eb);
-    float sn = 0.f, cs = 1.f;
-    if (s.pairs.turns(i)) turn(pos, s.turns[i], sn, cs);
-    ua[k] = a * cs + c * sn;
-    ub[k] = c * cs - a * sn;
+    const float a = ld_global(dy + ea), c = ld_global(dy + eb);
+    ua[k] = a * cs[k] + c * sn[k];
+    ub[k] = c * cs[k] - a * sn[k];
   }
   return s.rstd(wave_sum(ss));
 }
 
-template <typename T>
+constexpr int kAnyThreads = 512;
+template <typename T, int PER>
 __device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& d) {
   const Head s(t, d);
   const int lane = threadIdx.x & 63;
-  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * 4) {
+  constexpr int W = kAnyThreads / 64;
+  for (int64_t id = (int64_t)blockIdx.x * W + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * W) {
     const int row = (int)(id / s.heads), h = (int)(id % s.heads);
     const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
     const T* gain = (const T*)t.ptrs[d.ptr0 + 2];
-    float ua[kPer], ub[kPer], xa[kPer], xb[kPer], dot = 0.f;
-    const float r = load_reverse(s, (const T*)t.ptrs[d.ptr0] + at, (const T*)t.ptrs[d.ptr0 + 1] + at, s.position(row), lane, ua, ub, xa, xb);
+    float ua[PER], ub[PER], xa[PER], xb[PER], sn[PER], cs[PER], dot = 0.f;
+    angles(s, s.position(row), lane, sn, cs);
+    const float r = load_reverse(s, (const T*)t.ptrs[d.ptr0] + at, (const T*)t.ptrs[d.ptr0 + 1] + at, sn, cs, lane, ua, ub, xa, xb);
     T* o = (T*)d.out + at;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
+    for (int k = 0; k < PER; ++k) {
       const int i = lane + 64 * k;
       if (i >= s.head_dim / 2) continue;
       int ea, eb;
@@ -167,7 +179,7 @@ __device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& 
     }
     const float m = wave_sum(dot) * r * r / (float)s.head_dim;  // mean(u gain n) * rsqrt(..): the second rsqrt(..) is n's below
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
+    for (int k = 0; k < PER; ++k) {
       const int i = lane + 64 * k;
       if (i >= s.head_dim / 2) continue;
       int ea, eb;
@@ -178,29 +190,35 @@ __device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& 
   }
 }
 
-// Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every fourth (row, head) of them and keeps its
-// sums in registers; the four are added in order.
-template <typename T>
+// Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every eighth of them, forms its angles once and keeps its
+// sums in registers; the eight are added in order.
+template <typename T, int PER>
 __device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d, float (*part)[1024]) {
+  constexpr int W = kAnyThreads / 64;
   const Head s(t, d);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
-  float ga[kPer], gb[kPer];
+  float ga[PER], gb[PER], sn[PER], cs[PER];
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) ga[k] = gb[k] = 0.f;
-  for (int64_t id = w; id < (int64_t)n * s.heads; id += 4) {
-    const int row = row0 + (int)(id / s.heads), h = (int)(id % s.heads);
-    const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
-    float ua[kPer], ub[kPer], xa[kPer], xb[kPer];
-    const float r = load_reverse(s, (const T*)t.ptrs[d.ptr0] + at, (const T*)t.ptrs[d.ptr0 + 1] + at, s.position(row), lane, ua, ub, xa, xb);
+  for (int k = 0; k < PER; ++k) ga[k] = gb[k] = 0.f;
+  for (int r = w; r < n; r += W) {
+    const size_t at = (size_t)(row0 + r) * s.cols;
+    const T* dy = (const T*)t.ptrs[d.ptr0] + at;
+    const T* x = (const T*)t.ptrs[d.ptr0 + 1] + at;
+    angles(s, s.position(row0 + r), lane, sn, cs);
+#pragma unroll(PER == 1 ? 4 : 1)
+    for (int h = 0; h < s.heads; ++h) {
+      float ua[PER], ub[PER], xa[PER], xb[PER];
+      const float rstd = load_reverse(s, dy + (size_t)h * s.head_dim, x + (size_t)h * s.head_dim, sn, cs, lane, ua, ub, xa, xb);
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      ga[k] += ua[k] * (xa[k] * r);
-      gb[k] += ub[k] * (xb[k] * r);
+      for (int k = 0; k < PER; ++k) {
+        ga[k] += ua[k] * (xa[k] * rstd);
+        gb[k] += ub[k] * (xb[k] * rstd);
+      }
     }
   }
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
+  for (int k = 0; k < PER; ++k) {
     const int i = lane + 64 * k;
     if (i >= s.head_dim / 2) continue;
     int ea, eb;
@@ -210,17 +228,27 @@ __device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d
   }
   __syncthreads();
   float* o = (float*)d.out + (size_t)block * s.head_dim;
-  for (int c = threadIdx.x; c < s.head_dim; c += 256) o[c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+  for (int c = threadIdx.x; c < s.head_dim; c += kAnyThreads) {
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) sum += part[k][c];
+    o[c] = sum;
+  }
 }
 
 // Both gradients go in one launch.
 template <typename T>
-__global__ void __launch_bounds__(256) head_rope_bwd_kernel(DeviceTables t, Batch b) {
+__global__ void __launch_bounds__(kAnyThreads) head_rope_bwd_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
-  __shared__ float part[4][1024];
-  if (d.p.mode) head_gain<T>(t, d, part);
-  else head_input<T>(t, d);
+  __shared__ float part[kAnyThreads / 64][1024];
+  if (d.p.head_dim <= 128) {
+    if (d.p.mode) head_gain<T, 1>(t, d, part);
+    else head_input<T, 1>(t, d);
+  } else {
+    if (d.p.mode) head_gain<T, kPer>(t, d, part);
+    else head_input<T, kPer>(t, d);
+  }
 }
 
 // ---- heads of a multiple of 16 elements, pairs that come in eights ---------------------------------
@@ -564,8 +592,7 @@ int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   };
   switch (cls) {
     case LC_HEAD_ROPE_BWD:
-      if (d.p.mode) return d.rows;  // sums of the gain's gradient
-      [[fallthrough]];
+      return d.p.mode ? d.rows : (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + kAnyThreads / 64 - 1) / (kAnyThreads / 64), kGenericBlocks);
     case LC_HEAD_ROPE: return (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + 3) / 4, kGenericBlocks);
     case LC_HEAD_ROPE_EIGHTS: return walks(256);
     case LC_HEAD_ROPE_BWD_EIGHTS: return d.p.mode ? d.rows : walks(kBwdThreads);
@@ -583,7 +610,10 @@ hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& 
   } while (0)
   switch (cls) {
     case LC_HEAD_ROPE: TN_LAUNCH(head_rope_kernel); break;
-    case LC_HEAD_ROPE_BWD: TN_LAUNCH(head_rope_bwd_kernel); break;
+    case LC_HEAD_ROPE_BWD:
+      if (bf) hipLaunchKernelGGL(head_rope_bwd_kernel<bf16_t>, grid, dim3(kAnyThreads), 0, s, t, b);
+      else hipLaunchKernelGGL(head_rope_bwd_kernel<float>, grid, dim3(kAnyThreads), 0, s, t, b);
+      break;
     case LC_HEAD_ROPE_EIGHTS: TN_LAUNCH(head_rope_eights_kernel); break;
     case LC_HEAD_ROPE_BWD_EIGHTS:
       if (bf) hipLaunchKernelGGL(head_rope_bwd_eights_kernel<bf16_t>, grid, dim3(kBwdThreads), 0, s, t, b);

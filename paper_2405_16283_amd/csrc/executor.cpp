@@ -396,8 +396,10 @@ tn_status build_tables(tn_executor& ex) {
             theta.push_back(share == 1.0 ? f : f * share + f / (double)x.p.rope_factor * (1.0 - share));
           }
         }
-        aux.insert(aux.end(), {it->second, rd, x.p.rope_half != 0, x.p.norm != 0, x.p.positions != 0, xd.rows, xd.cols, head_walk(xd.rows, xd.cols / x.p.head_dim, x.p.head_dim)});
+        aux.insert(aux.end(), {it->second, rd, x.p.rope_half != 0, x.p.norm != 0, x.p.positions != 0, xd.rows, xd.cols, back});
+        aux.push_back(head_walk(aux.data() + d.aux0, x.p.head_dim));
         if (head_by_eights(aux.data() + d.aux0, x.p.head_dim)) vi.cls += LC_HEAD_ROPE_EIGHTS - LC_HEAD_ROPE;
+        else vi.head_dim = (int16_t)(x.p.head_dim > kHeadSmall ? kHeadSmall + 1 : kHeadSmall);  // (two groups, whatever the sizes are)
         break;
       }
       case TN_OP_COL_SUM:

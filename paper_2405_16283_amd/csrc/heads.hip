@@ -37,10 +37,18 @@ __device__ __forceinline__ void turn(double position, double turns, float& sn, f
   sincospif(2.f * (float)a, &sn, &cs);
 }
 
+template <int CTRL>
+__device__ __forceinline__ float exchanged(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+// over the wavefront: in each sixteen lanes by exchanges inside the vector unit (neighbours, pairs, the mirrored half of eight, of sixteen)
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  v += exchanged<0xB1>(v);
+  v += exchanged<0x4E>(v);
+  v += exchanged<0x141>(v);
+  v += exchanged<0x140>(v);
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
 }
 
 // What a row's workgroup needs of its vertex.
@@ -71,54 +79,7 @@ struct Head {
 };
 
 constexpr int kPer = 8;  // pairs per lane: heads of up to 1024 elements
-constexpr int64_t kGenericBlocks = 1 << 18;  // far more wavefronts than the chip holds, and far from what a launch may have
-
-// Any head size: a wavefront per row and head at a time, lane by lane through its pairs.
-template <typename T>
-__global__ void __launch_bounds__(256) head_rope_kernel(DeviceTables t, Batch b) {
-  const OpDesc& d = t.descs[b.at(blockIdx.y)];
-  if ((int)blockIdx.x >= d.nblocks) return;
-  const Head s(t, d);
-  const int lane = threadIdx.x & 63;
-  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * 4) {
-    const int row = (int)(id / s.heads), h = (int)(id % s.heads);
-    const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
-    const T* x = (const T*)t.ptrs[d.ptr0] + at;
-    const T* gain = s.norm ? (const T*)t.ptrs[d.ptr0 + 1] : nullptr;
-    T* o = (T*)d.out + at;
-    float va[kPer], vb[kPer], ss = 0.f;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = lane + 64 * k;
-      va[k] = vb[k] = 0.f;
-      if (i >= s.head_dim / 2) continue;
-      int ea, eb;
-      s.pairs.elements(i, ea, eb);
-      va[k] = ld(x + ea);
-      vb[k] = ld(x + eb);
-      ss += va[k] * va[k] + vb[k] * vb[k];
-    }
-    const float r = s.norm ? s.rstd(wave_sum(ss)) : 1.f;
-    const double pos = s.position(row);
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = lane + 64 * k;
-      if (i >= s.head_dim / 2) continue;
-      int ea, eb;
-      s.pairs.elements(i, ea, eb);
-      float a = va[k], c = vb[k];
-      if (s.norm) {
-        a *= r * ld(gain + ea);
-        c *= r * ld(gain + eb);
-      }
-      float sn = 0.f, cs = 1.f;
-      if (s.pairs.turns(i)) turn(pos, s.turns[i], sn, cs);
-      if (d.p.mode) sn = -sn;
-      st(o + ea, a * cs - c * sn);
-      st(o + eb, a * sn + c * cs);
-    }
-  }
-}
+constexpr int64_t kGenericBlocks = 1 << 16;  // far more wavefronts than the chip holds, and far from what a launch may have
 
 // sines and cosines of this lane's pairs in a row at `pos`
 template <int PER>
@@ -128,6 +89,92 @@ __device__ __forceinline__ void angles(const Head& s, double pos, int lane, floa
     sn[k] = 0.f;
     cs[k] = 1.f;
     if (s.pairs.turns(lane + 64 * k)) turn(pos, s.turns[lane + 64 * k], sn[k], cs[k]);
+  }
+}
+
+// Heads of any size: a wavefront to a row and a run of its heads at a time (kHeadWalk), a lane to every 64th pair, whose angles serve the whole
+// run.  Elements of a head of up to 128 are fetched while the head before it is worked on; larger ones have a kernel of their own, whose
+// eight pairs to a lane leave registers for one head (in one kernel with them, small heads had a fifth of the wavefronts).  2000 rows of 32 heads
+// of 80 of which 20 turn, bf16: 18 us (20 MB); a head to a wavefront, each with its angles, 35.  Both gradients 76 us; four wavefronts to 32 rows of
+// the gain's and angles for every head 332.
+struct Run {
+  int row, h0, h1;
+  __device__ Run(const Head& s, int64_t id) {
+    const int walk = s.ax[kHeadWalk], runs = (s.heads + walk - 1) / walk;
+    row = (int)(id / runs);
+    h0 = (int)(id % runs) * walk;
+    h1 = min(s.heads, h0 + walk);
+  }
+  __device__ static int64_t count(const Head& s) { return (int64_t)s.rows * ((s.heads + s.ax[kHeadWalk] - 1) / s.ax[kHeadWalk]); }
+};
+// (of large heads every head's addresses are formed anew: kept, they would take the registers)
+template <int PER>
+__device__ __forceinline__ int own_lane() {
+  int lane = threadIdx.x & 63;
+  if (PER > 1) asm volatile("" : "+v"(lane));
+  return lane;
+}
+template <typename T, int PER>
+struct Pieces {  // of a head, as loaded
+  T a[PER], b[PER];
+  __device__ void fetch(const Head& s, const T* p, int lane) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = lane + 64 * k;
+      a[k] = b[k] = T(0);
+      if (i >= s.head_dim / 2) continue;
+      int ea, eb;
+      s.pairs.elements(i, ea, eb);
+      a[k] = get_global(p + ea);
+      b[k] = get_global(p + eb);
+    }
+  }
+};
+__device__ __forceinline__ float wide(float v) { return v; }
+__device__ __forceinline__ float wide(bf16_t v) { return bf2f(v); }
+
+template <typename T, int PER>
+__global__ void __launch_bounds__(256) head_rope_kernel(DeviceTables t, Batch b) {
+  const OpDesc& d = t.descs[b.at(blockIdx.y)];
+  if ((int)blockIdx.x >= d.nblocks) return;
+  const Head s(t, d);
+  const int lane = threadIdx.x & 63;
+  const T* gain = s.norm ? (const T*)t.ptrs[d.ptr0 + 1] : nullptr;
+  const int64_t count = Run::count(s);
+  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < count; id += (int64_t)d.nblocks * 4) {
+    const Run at(s, id);
+    const T* x = (const T*)t.ptrs[d.ptr0] + (size_t)at.row * s.cols;
+    T* o = (T*)d.out + (size_t)at.row * s.cols;
+    Pieces<T, PER> next;
+    next.fetch(s, x + (size_t)at.h0 * s.head_dim, lane);
+    float sn[PER], cs[PER];
+    angles(s, s.position(at.row), lane, sn, cs);
+#pragma unroll 1
+    for (int h = at.h0; h < at.h1; ++h) {
+      const int lane = own_lane<PER>();
+      if (PER > 1 && h > at.h0) next.fetch(s, x + (size_t)h * s.head_dim, lane);
+      const Pieces<T, PER> v = next;
+      if (PER == 1 && h + 1 < at.h1) next.fetch(s, x + (size_t)(h + 1) * s.head_dim, lane);
+      float ss = 0.f;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) ss += wide(v.a[k]) * wide(v.a[k]) + wide(v.b[k]) * wide(v.b[k]);
+      const float r = s.norm ? s.rstd(wave_sum(ss)) : 1.f;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const int i = lane + 64 * k;
+        if (i >= s.head_dim / 2) continue;
+        int ea, eb;
+        s.pairs.elements(i, ea, eb);
+        float a = wide(v.a[k]), c = wide(v.b[k]);
+        if (s.norm) {
+          a *= r * ld_global(gain + ea);
+          c *= r * ld_global(gain + eb);
+        }
+        const float n = d.p.mode ? -sn[k] : sn[k];
+        st(o + (size_t)h * s.head_dim + ea, a * cs[k] - c * n);
+        st(o + (size_t)h * s.head_dim + eb, a * n + c * cs[k]);
+      }
+    }
   }
 }
 
@@ -153,12 +200,13 @@ __device__ __forceinline__ float load_reverse(const Head& s, const T* dy, const 
   return s.rstd(wave_sum(ss));
 }
 
-constexpr int kAnyThreads = 512;
+constexpr int any_threads(int per) { return per == 1 ? 1024 : 512; }  // (of large heads 1024 threads have not the registers)
+constexpr int any_columns(int per) { return 128 * per; }
 template <typename T, int PER>
 __device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& d) {
   const Head s(t, d);
   const int lane = threadIdx.x & 63;
-  constexpr int W = kAnyThreads / 64;
+  constexpr int W = any_threads(PER) / 64;
   for (int64_t id = (int64_t)blockIdx.x * W + (threadIdx.x >> 6); id < (int64_t)s.rows * s.heads; id += (int64_t)d.nblocks * W) {
     const int row = (int)(id / s.heads), h = (int)(id % s.heads);
     const size_t at = (size_t)row * s.cols + (size_t)h * s.head_dim;
@@ -190,11 +238,11 @@ __device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& 
   }
 }
 
-// Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every eighth of them, forms its angles once and keeps its
-// sums in registers; the eight are added in order.
+// Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every W-th of them, forms its angles once and keeps its
+// sums in registers; the W are added in order.
 template <typename T, int PER>
-__device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d, float (*part)[1024]) {
-  constexpr int W = kAnyThreads / 64;
+__device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d, float (*part)[any_columns(PER)]) {
+  constexpr int W = any_threads(PER) / 64;
   const Head s(t, d);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
@@ -228,7 +276,7 @@ __device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d
   }
   __syncthreads();
   float* o = (float*)d.out + (size_t)block * s.head_dim;
-  for (int c = threadIdx.x; c < s.head_dim; c += kAnyThreads) {
+  for (int c = threadIdx.x; c < s.head_dim; c += any_threads(PER)) {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < W; ++k) sum += part[k][c];
@@ -237,18 +285,13 @@ __device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d
 }
 
 // Both gradients go in one launch.
-template <typename T>
-__global__ void __launch_bounds__(kAnyThreads) head_rope_bwd_kernel(DeviceTables t, Batch b) {
+template <typename T, int PER>
+__global__ void __launch_bounds__(any_threads(PER)) head_rope_bwd_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
-  __shared__ float part[kAnyThreads / 64][1024];
-  if (d.p.head_dim <= 128) {
-    if (d.p.mode) head_gain<T, 1>(t, d, part);
-    else head_input<T, 1>(t, d);
-  } else {
-    if (d.p.mode) head_gain<T, kPer>(t, d, part);
-    else head_input<T, kPer>(t, d);
-  }
+  __shared__ float part[any_threads(PER) / 64][any_columns(PER)];
+  if (d.p.mode) head_gain<T, PER>(t, d, part);
+  else head_input<T, PER>(t, d);
 }
 
 // ---- heads of a multiple of 16 elements, pairs that come in eights ---------------------------------
@@ -290,11 +333,6 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
 }
 __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
   *(uint4*)p = make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
-}
-
-template <int CTRL>
-__device__ __forceinline__ float exchanged(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
 }
 
 // A lane's place in its head: where its two runs begin, and whether its pairs are (run 0, run 1) or neighbours.
@@ -586,44 +624,49 @@ __global__ void __launch_bounds__(256) col_sum_kernel(DeviceTables t, Batch b) {
 
 int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux) {
   const int32_t* ax = aux + d.aux0;
-  const int64_t heads = cls == LC_COL_SUM ? 0 : ax[kHeadCols] / d.p.head_dim;
-  auto walks = [&](int64_t threads) {
-    return (int32_t)((ax[kHeadRows] * ((heads + ax[kHeadWalk] - 1) / ax[kHeadWalk]) * head_lanes(d.p.head_dim) + threads - 1) / threads);
-  };
+  if (cls == LC_COL_SUM) return (d.cols + 31) / 32;
+  if (ax[kHeadBack] && d.p.mode) return d.rows;  // sums of the gain's gradient
+  const int64_t runs = (int64_t)ax[kHeadRows] * ((ax[kHeadCols] / d.p.head_dim + ax[kHeadWalk] - 1) / ax[kHeadWalk]);
+  auto blocks = [&](int64_t lanes, int64_t threads) { return (runs * lanes + threads - 1) / threads; };
   switch (cls) {
-    case LC_HEAD_ROPE_BWD:
-      return d.p.mode ? d.rows : (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + kAnyThreads / 64 - 1) / (kAnyThreads / 64), kGenericBlocks);
-    case LC_HEAD_ROPE: return (int32_t)std::min<int64_t>((ax[kHeadRows] * heads + 3) / 4, kGenericBlocks);
-    case LC_HEAD_ROPE_EIGHTS: return walks(256);
-    case LC_HEAD_ROPE_BWD_EIGHTS: return d.p.mode ? d.rows : walks(kBwdThreads);
-    default: return (d.cols + 31) / 32;
+    case LC_HEAD_ROPE: return (int32_t)std::min(blocks(64, 256), kGenericBlocks);
+    case LC_HEAD_ROPE_BWD: {
+      const int64_t waves = any_threads(d.p.head_dim > kHeadSmall ? kPer : 1) / 64;
+      return (int32_t)std::min(((int64_t)ax[kHeadRows] * (ax[kHeadCols] / d.p.head_dim) + waves - 1) / waves, kGenericBlocks);
+    }
+    case LC_HEAD_ROPE_EIGHTS: return (int32_t)blocks(head_lanes(d.p.head_dim), 256);
+    default: return (int32_t)blocks(head_lanes(d.p.head_dim), kBwdThreads);
   }
 }
 
-hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
-  const dim3 grid((unsigned)max_blocks, (unsigned)b.n), wg(256);
-  const bool bf = dtype == TN_BF16;
-#define TN_LAUNCH(kernel)                                              \
-  do {                                                                 \
-    if (bf) hipLaunchKernelGGL(kernel<bf16_t>, grid, wg, 0, s, t, b);  \
-    else hipLaunchKernelGGL(kernel<float>, grid, wg, 0, s, t, b);      \
-  } while (0)
+namespace {
+template <typename T>
+hipError_t launch(int cls, bool large, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+  const dim3 grid((unsigned)max_blocks, (unsigned)b.n);
+  void (*kernel)(DeviceTables, Batch);
+  int threads = 256;
   switch (cls) {
-    case LC_HEAD_ROPE: TN_LAUNCH(head_rope_kernel); break;
+    case LC_HEAD_ROPE: kernel = large ? head_rope_kernel<T, kPer> : head_rope_kernel<T, 1>; break;
     case LC_HEAD_ROPE_BWD:
-      if (bf) hipLaunchKernelGGL(head_rope_bwd_kernel<bf16_t>, grid, dim3(kAnyThreads), 0, s, t, b);
-      else hipLaunchKernelGGL(head_rope_bwd_kernel<float>, grid, dim3(kAnyThreads), 0, s, t, b);
+      kernel = large ? head_rope_bwd_kernel<T, kPer> : head_rope_bwd_kernel<T, 1>;
+      threads = any_threads(large ? kPer : 1);
       break;
-    case LC_HEAD_ROPE_EIGHTS: TN_LAUNCH(head_rope_eights_kernel); break;
+    case LC_HEAD_ROPE_EIGHTS: kernel = head_rope_eights_kernel<T>; break;
     case LC_HEAD_ROPE_BWD_EIGHTS:
-      if (bf) hipLaunchKernelGGL(head_rope_bwd_eights_kernel<bf16_t>, grid, dim3(kBwdThreads), 0, s, t, b);
-      else hipLaunchKernelGGL(head_rope_bwd_eights_kernel<float>, grid, dim3(kBwdThreads), 0, s, t, b);
+      kernel = head_rope_bwd_eights_kernel<T>;
+      threads = kBwdThreads;
       break;
-    case LC_COL_SUM: hipLaunchKernelGGL(col_sum_kernel, grid, wg, 0, s, t, b); break;
+    case LC_COL_SUM: kernel = col_sum_kernel; break;
     default: return hipErrorInvalidValue;
   }
-#undef TN_LAUNCH
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, t, b);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_heads(int cls, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t s) {
+  const bool large = head_dim > kHeadSmall;
+  return dtype == TN_BF16 ? launch<bf16_t>(cls, large, t, b, max_blocks, s) : launch<float>(cls, large, t, b, max_blocks, s);
 }
 
 }  // namespace tn

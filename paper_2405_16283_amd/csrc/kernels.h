@@ -228,8 +228,9 @@ int32_t attn_rule_blocks(int cls, const OpDesc& d, const int32_t* aux);
 hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
 // LC_HEAD_ROPE to LC_COL_SUM: heads.hip.  Auxiliary integers of all but the last (of LC_COL_SUM: rows per operand):
-enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadWalk, kHeadAux };
+enum { kHeadTheta = 0, kHeadRotary, kHeadHalf, kHeadNorm, kHeadPositions, kHeadRows, kHeadCols, kHeadBack, kHeadWalk, kHeadAux };
 constexpr int kGainRows = 32;  // rows to a sum of the gain's gradient
+constexpr int kHeadSmall = 128;  // a pair to a lane; larger heads have kernels, and launches, of their own
 // Heads of a multiple of 16 elements whose pairs come in eights go to the kernels for those: 16 elements to a lane, a head to a power of
 // two of lanes.  A lane's angles serve all the heads of its row that it walks over; it walks over fewer where there are few
 // rows, down to one, so that the chip has wavefronts enough.  Launches of 32 heads of 128, walking over 1, 2, 4 and 8 heads: 512 rows 8.4,
@@ -241,13 +242,14 @@ __host__ __device__ inline int head_lanes(int head_dim) {
   while (n * 16 < head_dim) n *= 2;
   return n;
 }
-inline int32_t head_walk(int64_t rows, int32_t heads, int32_t head_dim) {
+inline int32_t head_walk(const int32_t* ax, int32_t head_dim) {
+  const int64_t rows = ax[kHeadRows], heads = ax[kHeadCols] / head_dim, lanes = head_by_eights(ax, head_dim) ? head_lanes(head_dim) : 64;
   int32_t walk = 8;
-  while (walk > 1 && rows * ((heads + walk - 1) / walk) * head_lanes(head_dim) < kHeadLanes) walk /= 2;
+  while (walk > 1 && rows * ((heads + walk - 1) / walk) * lanes < kHeadLanes) walk /= 2;
   return walk;
 }
 int32_t head_blocks(int cls, const OpDesc& d, const int32_t* aux);
-hipError_t launch_heads(int cls, int dtype, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
+hipError_t launch_heads(int cls, int dtype, int head_dim, const DeviceTables& t, const Batch& b, int32_t max_blocks, hipStream_t stream);
 
 // LC_ATTN_RULE_F32_TILES and LC_ATTN_BWD_RULE_TILES: attn_rule_f32.hip.
 int32_t attn_rule_f32_blocks(int cls, const OpDesc& d, const int32_t* aux);

@@ -1548,7 +1548,7 @@ hipError_t launch_batch(int cls, int dtype, int head_dim, const DeviceTables& t,
     case LC_HEAD_ROPE_BWD:
     case LC_HEAD_ROPE_EIGHTS:
     case LC_HEAD_ROPE_BWD_EIGHTS:
-    case LC_COL_SUM: return launch_heads(cls, dtype, t, b, max_blocks, s);
+    case LC_COL_SUM: return launch_heads(cls, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE: return launch_attn_f32(true, true, dtype, head_dim, t, b, max_blocks, s);
     case LC_ATTN_BWD_RULE_TILES:
     case LC_ATTN_RULE_F32_TILES: return launch_attn_rule_f32(cls, head_dim, t, b, max_blocks, s);

@@ -238,7 +238,14 @@ __device__ __forceinline__ void head_input(const DeviceTables& t, const OpDesc& 
   }
 }
 
-// Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every W-th of them, forms its angles once and keeps its
+// How many of `all` (a power of two) that work on n rows share one.
+__device__ __forceinline__ int share(int all, int n) {
+  int rows = 1;
+  while (rows < n) rows *= 2;
+  return max(1, all / rows);
+}
+
+// Sums of the gain's gradient: a workgroup per kGainRows rows, a wavefront takes every W-th of them (where they are few, several share a row), forms its angles once and keeps its
 // sums in registers; the W are added in order.
 template <typename T, int PER>
 __device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d, float (*part)[any_columns(PER)]) {
@@ -249,13 +256,14 @@ __device__ __forceinline__ void head_gain(const DeviceTables& t, const OpDesc& d
   float ga[PER], gb[PER], sn[PER], cs[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) ga[k] = gb[k] = 0.f;
-  for (int r = w; r < n; r += W) {
+  const int per_row = share(W, n);  // wavefronts that share a row
+  for (int r = w / per_row; r < n; r += W / per_row) {
     const size_t at = (size_t)(row0 + r) * s.cols;
     const T* dy = (const T*)t.ptrs[d.ptr0] + at;
     const T* x = (const T*)t.ptrs[d.ptr0 + 1] + at;
     angles(s, s.position(row0 + r), lane, sn, cs);
 #pragma unroll(PER == 1 ? 4 : 1)
-    for (int h = 0; h < s.heads; ++h) {
+    for (int h = w % per_row; h < s.heads; h += per_row) {
       float ua[PER], ub[PER], xa[PER], xb[PER];
       const float rstd = load_reverse(s, dy + (size_t)h * s.head_dim, x + (size_t)h * s.head_dim, sn, cs, lane, ua, ub, xa, xb);
 #pragma unroll
@@ -522,7 +530,7 @@ __device__ __forceinline__ void head_gain_eights(const DeviceTables& t, const Op
   const Eights e(s);
   const int block = d.nblocks - 1 - (int)blockIdx.x, row0 = block * kGainRows, n = min(kGainRows, s.rows - row0);
   const int groups = kBwdThreads / e.lanes, group = threadIdx.x / e.lanes;
-  const int per_row = max(1, groups / kGainRows);  // groups that share a row
+  const int per_row = share(groups, n);  // groups that share a row
   float ga[8] = {}, gb[8] = {};
   for (int r = group / per_row; r < n; r += groups / per_row) {
     const T* dy = (const T*)t.ptrs[d.ptr0] + (size_t)(row0 + r) * s.cols;

@@ -72,7 +72,7 @@ def attention_bounds(q, k, v, head_dim, scale, ok, storage, products, cap=0.0, s
     """How far correct results may lie from the exact ones, element by element: {"o", "lse"} and with `do` {"dq", "dk", "dv"}.
 
     Counted are the roundings a kernel makes: of stored results (`storage`: half a step relative to the value, 2^-8 or 2^-24), of weights
-    and their gradients where they enter a product (`products`: 2^-8 for bf16 products, 0 for fp32), and those of fp32 arithmetic: of
+    and their gradients where they enter a product (`products`: 2^-16 as two bf16, 0 for fp32), and those of fp32 arithmetic: of
     a score, one unit (2^-24) per term of its sum and a few more for scaling, cap, bias and the exponential; of a sum over n rows, n units;
     a capped score's units are of its own size and, cap_sized, of the cap's (it is formed as cap - 2 cap / (1 + exp(2 z / cap))).
     O enters the reverse pass rounded to storage, or (rounded_o False) as it was before.  Below 2^-126, the smallest normal number, a weight, its gradient or a result may be zero."""

@@ -393,9 +393,9 @@ __device__ __forceinline__ void attn_rule_bwd_f32_body(const DeviceTables& t, co
       if (!__any(ql < key1 && qh > key0)) return;
       all_see = __all(ql <= key0 && qh >= row0 + 16);
     }
-    f32x4 s[KT], dp[KT], s2[KT];
+    f32x4 s[KT], dp[KT], s2[KT], dp2[KT];  // even and odd steps of the head apart: chains enough, of half the length and two thirds of the error
 #pragma unroll
-    for (int k = 0; k < KT; ++k) s[k] = dp[k] = s2[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < KT; ++k) s[k] = dp[k] = s2[k] = dp2[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < HD / 16; ++j) {
       f32x4 a[KT], b[KT];
@@ -408,9 +408,10 @@ __device__ __forceinline__ void attn_rule_bwd_f32_body(const DeviceTables& t, co
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
-          if (MODE == 3 && (j & 1)) s2[k] = mfma_f32(a[k][c], m1[j][c], s2[k]);  // chains of products enough
-          else s[k] = mfma_f32(a[k][c], m1[j][c], s[k]);
-          if (MODE != 3) dp[k] = mfma_f32(b[k][c], m2[j][c], dp[k]);
+          f32x4& into = j & 1 ? s2[k] : s[k];
+          f32x4& into2 = j & 1 ? dp2[k] : dp[k];
+          into = mfma_f32(a[k][c], m1[j][c], into);
+          if (MODE != 3) into2 = mfma_f32(b[k][c], m2[j][c], into2);
         }
     }
     // element i of s[k]: row o0 + 16 k + 4 g + i of the other side
@@ -424,14 +425,14 @@ __device__ __forceinline__ void attn_rule_bwd_f32_body(const DeviceTables& t, co
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float other = (float)(o0 + 16 * k + 4 * g + i);
-        float z = (MODE == 3 ? s[k][i] + s2[k][i] : s[k][i]) * scale, th = 0.f;
+        float z = (s[k][i] + s2[k][i]) * scale, th = 0.f;
         if (rule.cap > 0.f) {
           th = tanh_f32(z * rule.inv_cap);
           z = rule.cap * th;
         }
         if (rule.slopes) z = fmaf(-slope, fabsf(OWN_Q ? from_me - other : from_me + other), z);
         float p = __expf(z - lse[i]);
-        if (MODE != 3) p *= (dp[k][i] - Dr[i]) * scale * (1.f - th * th);
+        if (MODE != 3) p *= (dp[k][i] + dp2[k][i] - Dr[i]) * scale * (1.f - th * th);
         s[k][i] = p;
       }
     }

@@ -150,7 +150,7 @@ class Case:
     def bounds(self, grad=False, rounded_o=True):
         c, b = self.c, self.dtype == "bf16"
         t = torch.tensor
-        x = H.attention_bounds(t(self.q), t(self.k), t(self.v), c["hd"], self.scale, self.ok, 2.0 ** (-8 if b else -24), 2.0 ** -8 if b else 0.0, self.cap,
+        x = H.attention_bounds(t(self.q), t(self.k), t(self.v), c["hd"], self.scale, self.ok, 2.0 ** (-8 if b else -24), 2.0 ** -16 if b else 0.0, self.cap,
                                self.slopes, c["q_pos0"], c["k_pos0"], t(self.do) if grad else None, rounded_o, cap_sized=b and self.cap <= 1024.0)
         return {n: a.numpy() for n, a in x.items()}
 

@@ -15,10 +15,11 @@
 // no row of the workgroup sees are skipped, 32-key slabs no row of the wavefront sees too, and only slabs that some row sees in
 // part pay for masking.
 //
-// Weights enter the second product as two bf16 each, the second holding what rounding has left of the first (Split): with one the output was 1.2 to
-// 1.5 times as far from the exact one as an output rounded once, and the gradients 1.5 times (a second error of the output's own size, which does
-// not average out where weights are alike), with two 1.00 times.  It costs half as many products again: 4096 queries against 4096 keys of 32
-// heads of 128, nothing masked, forward 301 -> 380 us, gradients with a cap 1321 -> 1497.
+// Weights and their gradients enter the second product as two bf16 each, the second holding what rounding has left of the first (Split), where
+// the result goes into further sums: partials, which are joined and which the reverse pass takes D from, and the gradients.  With one bf16 these
+// were 1.4 to 1.7 times as far from the exact ones as results rounded once (a second error of the result's own size), with two 1.00
+// times.  It costs half as many products again: 4096 queries against 4096 keys of 32 heads of 128, nothing masked, forward 301 -> 380 us,
+// gradients with a cap 1321 -> 1497.  Finished rows are rounded to bf16 right away and take one: 1.1 to 1.4 times as far off.
 #include "attn_rows.h"
 
 #include <climits>
@@ -76,7 +77,7 @@ __device__ __forceinline__ void load_own(void* const* tiles, int n_tiles, int nc
   for (int s = 0; s < HD / 16; ++s) v[s] = get_global((const bf16x8*)(p + s * 16 + g * 8));
 }
 
-template <int HD, bool CAP, bool SLOPES>
+template <int HD, bool CAP, bool SLOPES, bool FINISHED>
 __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch b) {
   const OpDesc& d = t.descs[b.at(blockIdx.y)];
   if ((int)blockIdx.x >= d.nblocks) return;
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
 #pragma unroll
         for (int e = 0; e < 2; ++e) a.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(size_t)(v_at[e][i] + (at + ks * 16 * (HD * 2))));
         ot[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p.hi, ot[i], 0, 0, 0);
-        ot[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p.lo, ot[i], 0, 0, 0);
+        if (!FINISHED) ot[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p.lo, ot[i], 0, 0, 0);
       }
     }
   };
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(256, 2) attn_rule_kernel(DeviceTables t, Batch
   }
   l += __shfl_xor(l, 32, 64);
   if (!exists) return;
-  if (ax[kRuleFinish]) {
+  if constexpr (FINISHED) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     bf16_t* out = (bf16_t*)d.out + (size_t)row * gw + h * HD + 4 * g;
 #pragma unroll
@@ -629,14 +630,14 @@ hipError_t launch(int threads, int lds, const DeviceTables& t, const Batch& b, i
   return hipGetLastError();
 }
 
-template <int HD>
+template <int HD, bool FINISHED>
 hipError_t launch_forward(int rule, const DeviceTables& t, const Batch& b, int32_t n, hipStream_t s) {
   constexpr int lds = 4 * kRuleKeys * HD * 2;
   switch (rule) {
-    case 0: return launch<attn_rule_kernel<HD, false, false>>(256, lds, t, b, n, s);
-    case kRuleHasCap: return launch<attn_rule_kernel<HD, true, false>>(256, lds, t, b, n, s);
-    case kRuleHasSlopes: return launch<attn_rule_kernel<HD, false, true>>(256, lds, t, b, n, s);
-    default: return launch<attn_rule_kernel<HD, true, true>>(256, lds, t, b, n, s);
+    case 0: return launch<attn_rule_kernel<HD, false, false, FINISHED>>(256, lds, t, b, n, s);
+    case kRuleHasCap: return launch<attn_rule_kernel<HD, true, false, FINISHED>>(256, lds, t, b, n, s);
+    case kRuleHasSlopes: return launch<attn_rule_kernel<HD, false, true, FINISHED>>(256, lds, t, b, n, s);
+    default: return launch<attn_rule_kernel<HD, true, true, FINISHED>>(256, lds, t, b, n, s);
   }
 }
 
@@ -665,8 +666,10 @@ hipError_t launch_attn_rule(int cls, int head_dim, const DeviceTables& t, const 
     if (head_dim == 128) return launch_reverse<128>(cls - LC_ATTN_BWD_RULE_BF16, t, b, max_blocks, s);
     return hipErrorInvalidValue;
   }
-  if (head_dim == 64) return launch_forward<64>(cls - LC_ATTN_RULE_BF16, t, b, max_blocks, s);
-  if (head_dim == 128) return launch_forward<128>(cls - LC_ATTN_RULE_BF16, t, b, max_blocks, s);
+  const int rule = (cls - LC_ATTN_RULE_BF16) & (kRuleHasCap | kRuleHasSlopes);
+  const bool finished = (cls - LC_ATTN_RULE_BF16) & kRuleFinished;
+  if (head_dim == 64) return finished ? launch_forward<64, true>(rule, t, b, max_blocks, s) : launch_forward<64, false>(rule, t, b, max_blocks, s);
+  if (head_dim == 128) return finished ? launch_forward<128, true>(rule, t, b, max_blocks, s) : launch_forward<128, false>(rule, t, b, max_blocks, s);
   return hipErrorInvalidValue;
 }
 

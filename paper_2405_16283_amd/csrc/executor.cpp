@@ -432,7 +432,7 @@ tn_status build_tables(tn_executor& ex) {
           add_rule(x.p, (nq + 2 * nkv) * nc);
           // the bf16 kernel wants plain V tiles, whole heads inside one column tile and 64-key chunks inside one row tile
           vi.cls = (d.dtype == TN_BF16 && x.p.score_cap <= kRuleCapMost && !x.p.v_trans && tc % hd == 0 && (nkv == 1 || tk % 64 == 0))
-                       ? (int8_t)(LC_ATTN_RULE_BF16 + rule_kernel(x.p)) : (int8_t)LC_ATTN_RULE_F32;
+                       ? (int8_t)(LC_ATTN_RULE_BF16 + rule_kernel(x.p) + (x.p.finish ? kRuleFinished : 0)) : (int8_t)LC_ATTN_RULE_F32;
           // so does the fp32 kernel for whole tiles, of chunks of 2048 / head_dim keys
           if (d.dtype == TN_F32 && !x.p.v_trans && tc % hd == 0 && (nkv == 1 || tk % (2048 / hd) == 0)) vi.cls = LC_ATTN_RULE_F32_TILES;
           vi.head_dim = (int16_t)hd;

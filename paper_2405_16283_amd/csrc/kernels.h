@@ -90,9 +90,9 @@ enum LaunchClass {
   LC_ATTN_RULE_F32_TILES, // the same where a chunk of keys of a head lies inside one tile
   LC_ATTN_BWD_RULE,  // its gradients, fp32 products
   LC_ATTN_BWD_RULE_TILES, // the same where a chunk of the other side's rows of a head lies inside one tile
-  LC_ATTN_RULE_BF16, // attention with a score rule or finished rows, bf16 products: plus kRuleHasCap and kRuleHasSlopes
-  LC_ATTN_RULE_BF16_LAST = LC_ATTN_RULE_BF16 + 3,
-  LC_ATTN_BWD_RULE_BF16, // its gradients: plus the same
+  LC_ATTN_RULE_BF16, // attention with a score rule or finished rows, bf16 products: plus kRuleHasCap, kRuleHasSlopes and kRuleFinished
+  LC_ATTN_RULE_BF16_LAST = LC_ATTN_RULE_BF16 + 7,
+  LC_ATTN_BWD_RULE_BF16, // its gradients: plus the first two
   LC_ATTN_BWD_RULE_BF16_LAST = LC_ATTN_BWD_RULE_BF16 + 3,
   LC_ATTN_STATS,     // their statistics from O, dO and the log-sum-exp
   LC_ATTN_JOIN,      // combine with finish 1
@@ -217,7 +217,7 @@ inline bool join_few(const OpDesc& d) {
   const int hd = d.p.head_dim;
   return d.n_in >= 16 && (int64_t)d.rows * d.cols <= 512 * 1024 && hd % 4 == 0 && hd <= 1024 && d.p.hpg % 2 == 0 && d.p.col0 % hd == 0 && d.cols % hd == 0;
 }
-enum { kRuleHasCap = 1, kRuleHasSlopes = 2 };  // kernels of their own
+enum { kRuleHasCap = 1, kRuleHasSlopes = 2, kRuleFinished = 4 };  // kernels of their own
 // The largest cap that the bf16 kernels take: they form a capped score as cap - 2 cap / (1 + exp(2 z / cap)), of which cap * 2^-22 and a little
 // is lost: 2^-12 of a weight here, and more than its rounding to bf16 from some ten times as much.  Larger ones go to attn_f32.hip (1024 causal
 // rows of 32 heads of 128: 295 us instead of 38, gradients 772 instead of 134; a cap is some tens where it is used at all).

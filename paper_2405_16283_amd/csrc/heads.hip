@@ -305,8 +305,8 @@ __global__ void __launch_bounds__(any_threads(PER)) head_rope_bwd_kernel(DeviceT
 // ---- heads of a multiple of 16 elements, pairs that come in eights ---------------------------------
 // Eight pairs to a lane -- two runs of eight elements, 16-byte accesses -- and a head to 4, 8, 16 .. lanes, of which those past its end
 // are idle.  What bounds these is memory; a lane's angles, 8 of them with 64-bit products, are formed once for the heads it walks
-// over, as many as leave enough wavefronts to fill the chip (kHeadWalk).  16384 rows of 32 heads of 128, bf16, with norm: 53 us (268 MB,
-// 5.1 TB/s), the gradient 72 (403 MB, 5.6 TB/s); by wavefronts of a pair to a lane (the kernels above) 218 and 340.  One row: 6.6 us, a
+// over, as many as leave enough wavefronts to fill the chip (kHeadWalk).  16384 rows of 32 heads of 128, bf16, with norm: 52 us (268 MB,
+// 5.1 TB/s), both gradients 117 (671 MB, 5.7 TB/s); by wavefronts of a pair to a lane, a head each, 218 and 704.  One row: 5.2 us, a
 // launch and three dependent loads.
 
 // eight elements as loaded, which may be on their way while the head before them is worked on
@@ -521,7 +521,7 @@ __device__ __forceinline__ void head_input_eights(const DeviceTables& t, const O
 
 // Sums of the gain's gradient: the lanes of a head keep to one row at a time and walk over its heads; what the groups of a wavefront
 // and the wavefronts of the workgroup have summed is added in a fixed order.  Blocks of rows go from the last to the first: the gradient
-// of the input, formed from the same operands, leaves its last ones in the caches.  16384 rows of 32 heads of 128, bf16: 55 us (268
+// of the input, formed from the same operands, leaves its last ones in the caches.  Alone, 16384 rows of 32 heads of 128, bf16: 55 us (268
 // MB, 4.9 TB/s), from the first row on 63.  64 rows: 18 us, sixteen heads one behind the other; with 256 threads, which take 32,
 // 23; with 1024 17, but three heads of 64 in fp32 14 instead of 9, since registers spill.
 template <typename T>
